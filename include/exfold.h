@@ -375,6 +375,111 @@ exfold_status exfold_calibrate_diagonal(const exfold_layer *layer, const void *x
                                         double lambda, int32_t mode, float *Dg, float *Ld, void *ws,
                                         size_t ws_bytes, void *stream);
 
+/*
+ * Routing of tokens to experts from router logits: the step before
+ * exfold_select_prefill / exfold_select_decode_pool (which take its routes with
+ * logits == NULL) and exfold_moe_execute, for routers other than the Top-K softmax
+ * of Eq. topk_gate.
+ *
+ * Scores.   SOFTMAX: p_e = exp(l_e) / sum over all N experts; SIGMOID: p_e =
+ *           1 / (1 + exp(-l_e)).  A logit of -infinity or NaN masks its expert (p_e =
+ *           0); +infinity counts as the largest finite value.
+ * Values.   What the selection compares: v_e = l_e without select_bias (both scores
+ *           grow with the logit), v_e = p_e + select_bias[e] with it (in float64).  The
+ *           bias steers the selection only, never a weight; a bias of -infinity or NaN
+ *           masks its expert for every token (a softmax still counts its logit).
+ * Groups.   N / n_groups consecutive experts each.  The value of a group is the
+ *           largest v_e (MAX) or the sum of its two largest p_e + select_bias[e]
+ *           (TOP2; the bias 0 when NULL; masked experts add nothing).  The keep_groups
+ *           groups of largest value stay, equal values by group id; a group without an
+ *           unmasked expert comes last.
+ * Routes.   The first K experts of those groups by (v_e descending, id ascending),
+ *           masked experts last by id: a token with fewer than K unmasked ones is
+ *           filled up with masked ones.
+ * Weights.  p_e (0 for a masked expert); with renorm divided by their sum over the K
+ *           routes (all 0 when that sum is 0); times scale.  Evaluated in float64 and
+ *           rounded once to float32.
+ */
+enum { EXFOLD_SCORE_SOFTMAX = 0, EXFOLD_SCORE_SIGMOID = 1 };
+enum { EXFOLD_GROUP_MAX = 0, EXFOLD_GROUP_TOP2 = 1 };
+
+typedef struct exfold_routing {
+  int32_t score;             /* EXFOLD_SCORE_*                                     */
+  int32_t group_value;       /* EXFOLD_GROUP_*                                     */
+  int64_t n_groups;          /* divides N; 1 = no groups                           */
+  int64_t keep_groups;       /* 1 .. n_groups, keep_groups * (N / n_groups) >= K    */
+  int32_t renorm;            /* nonzero: the K weights are divided by their sum    */
+  float scale;               /* finite, > 0; the decode pool's exact sums hold
+                                while T * scale < 2^23                             */
+  const float *select_bias;  /* [N] float32 device, or NULL                        */
+} exfold_routing;
+
+/*
+ *   logits   [T, N] of dtype (EXFOLD_F32 or EXFOLD_BF16), rows ld >= N elements apart.
+ *   topk_ids [T, K] int32, topk_w [T, K] float32 outputs (neither may overlap the
+ *            logits, the bias or each other: EXFOLD_ERR_ARG).
+ * Limits and no-op as above (T <= 2^22).  Errors: EXFOLD_ERR_ARG for an unknown score or
+ * group value, a scale that is not finite and positive, or overlapping buffers;
+ * EXFOLD_ERR_SHAPE for groups that do not divide N or hold fewer than K experts;
+ * EXFOLD_ERR_ALIGN for pointers not aligned to their element.
+ */
+exfold_status exfold_route_experts(const exfold_routing *routing, const void *logits, int32_t dtype,
+                                   int64_t ld, int64_t T, int64_t N, int64_t K, int32_t *topk_ids,
+                                   float *topk_w, void *stream);
+
+/*
+ * Matrix product with bias, activation and residual in its epilogue: the router's
+ * logits in float32, shared experts of another width than the routed ones, the MLP of
+ * the layers that have no experts.
+ *   y = act(x W^T + b) + r
+ *   gated:  y = act(x W_g^T + b_g) * (x W_u^T + b_u) + r,  W_g the first n_out rows of
+ *           w and W_u the next n_out (the layout of exfold_layer.ws_gate_up).
+ * Sums in float32, one rounding to out_dtype.
+ *   ACT_SILU: z / (1 + e^-z); ACT_GELU: z Phi(z); ACT_GELU_TANH: z (1 + tanh(sqrt(2/pi)
+ *   (z + 0.044715 z^3))) / 2.
+ */
+enum {
+  EXFOLD_ACT_NONE = 0,
+  EXFOLD_ACT_RELU = 1,
+  EXFOLD_ACT_SILU = 2,
+  EXFOLD_ACT_GELU = 3,
+  EXFOLD_ACT_GELU_TANH = 4
+};
+
+typedef struct exfold_linear {
+  int64_t n_in;       /* reduction length, 1 .. 2^17                               */
+  int64_t n_out;      /* output columns, 1 .. 2^17                                 */
+  int64_t ldw;        /* elements between rows of w, n_in .. 2^31                  */
+  const void *w;      /* [n_out, n_in] of dtype; gated: [2 n_out, n_in]            */
+  const float *bias;  /* [n_out] (gated [2 n_out]) float32, or NULL                */
+  int32_t dtype;      /* of x and w                                                */
+  int32_t out_dtype;  /* of r and y: dtype, or EXFOLD_F32                          */
+  int32_t act;        /* EXFOLD_ACT_*                                              */
+  int32_t gated;      /* 0 or 1                                                    */
+} exfold_linear;
+
+/* Bytes of workspace exfold_linear_forward needs for M rows (at least 256), or 0 on
+ * invalid input.  Needed for its partial sums only, so calls that overlap in time (other
+ * streams, graphs replayed together) need workspaces of their own. */
+size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M);
+
+/*
+ *   x [M, n_in] rows ldx apart; residual [M, n_out] of out_dtype rows ldr apart, or NULL;
+ *   y [M, n_out] rows ldy apart (strides in elements, at least the row's length, at most
+ *   2^31; the gaps between rows are neither read nor written).  y may be the residual
+ *   itself (same pointer and stride: y += ...); any other overlap of y with an input or
+ *   the workspace is EXFOLD_ERR_ARG.
+ * Any sizes, strides and element-aligned pointers are valid; rows of x and w that start on
+ * 16 bytes and hold a whole number of 16-byte pieces are read in 16-byte vectors and run
+ * fastest.  M == 0 is a no-op; M <= 2^22, M * n_out <= 2^34 (else EXFOLD_ERR_SHAPE).
+ * Errors: EXFOLD_ERR_DTYPE for an unknown dtype or a bf16 output of float32 inputs;
+ * EXFOLD_ERR_ARG for an unknown activation or gate flag; EXFOLD_ERR_ALIGN for pointers not
+ * aligned to their element.
+ */
+exfold_status exfold_linear_forward(const exfold_linear *linear, const void *x, int64_t ldx, int64_t M,
+                                    const void *residual, int64_t ldr, void *y, int64_t ldy, void *ws,
+                                    size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

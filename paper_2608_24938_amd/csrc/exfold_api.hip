@@ -754,3 +754,151 @@ exfold_status exfold_gemm_plan(const exfold_layer *L, int64_t rows, int64_t acti
 }
 
 }  // extern "C"
+
+namespace {
+
+// Whether two strided matrices (rows of `width` bytes, `ld` bytes apart) share memory.
+// Equal strides: by the rows' column ranges (column slices of one buffer do not);
+// else by the ranges they span.
+struct Extent {
+  uintptr_t at;
+  int64_t rows, ld, width;  // bytes
+};
+bool overlap(const Extent &a, const Extent &b) {
+  if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0) return false;
+  const uintptr_t ea = a.at + (a.rows - 1) * a.ld + a.width, eb = b.at + (b.rows - 1) * b.ld + b.width;
+  if (ea <= b.at || eb <= a.at) return false;
+  if (a.ld != b.ld || a.rows == 1 || b.rows == 1) return true;
+  const int64_t l = a.ld, off = b.at >= a.at ? (int64_t)((b.at - a.at) % l) : (l - (int64_t)((a.at - b.at) % l)) % l;
+  return off < a.width || off + b.width > l;
+}
+inline Extent extent(const void *p, int64_t rows, int64_t ld, int64_t cols, int64_t esz) {
+  return Extent{reinterpret_cast<uintptr_t>(p), rows, ld * esz, cols * esz};
+}
+inline bool unaligned_to(const void *p, size_t esz) { return reinterpret_cast<uintptr_t>(p) % esz != 0; }
+inline size_t element(int32_t dtype) { return dtype == EXFOLD_BF16 ? 2 : 4; }
+
+constexpr int64_t kMaxWidth = int64_t(1) << 17;  // columns of x, w and y of a linear
+constexpr int64_t kMaxStride = int64_t(1) << 31;
+
+exfold_status check_linear(const exfold_linear *L, int64_t M) {
+  if (!L) return EXFOLD_ERR_NULL;
+  if ((L->dtype != EXFOLD_F32 && L->dtype != EXFOLD_BF16) ||
+      (L->out_dtype != L->dtype && L->out_dtype != EXFOLD_F32))
+    return EXFOLD_ERR_DTYPE;
+  if (L->act < EXFOLD_ACT_NONE || L->act > EXFOLD_ACT_GELU_TANH || (L->gated != 0 && L->gated != 1))
+    return EXFOLD_ERR_ARG;
+  if (L->n_in < 1 || L->n_out < 1 || L->n_in > kMaxWidth || L->n_out > kMaxWidth) return EXFOLD_ERR_SHAPE;
+  if (L->ldw < L->n_in || L->ldw > kMaxStride) return EXFOLD_ERR_SHAPE;
+  if (M < 0 || M > kMaxTokens || M * L->n_out > (int64_t(1) << 34)) return EXFOLD_ERR_SHAPE;
+  if (!L->w) return EXFOLD_ERR_NULL;
+  if (unaligned_to(L->w, element(L->dtype)) || unaligned_to(L->bias, 4)) return EXFOLD_ERR_ALIGN;
+  return EXFOLD_OK;
+}
+
+size_t linear_need(const exfold_linear *L, int64_t M) {
+  size_t need = kAlign;
+  for (int vec = 0; vec < 2; ++vec) {  // what the pointers and strides of the call allow
+    const LinearPlan p = plan_linear(L->dtype, L->gated != 0, vec != 0, (int)M, (int)L->n_out, (int)L->n_in, cu_count());
+    if (p.ksplit > 1) {
+      const size_t bytes = sizeof(float) * (size_t)p.ksplit * M * linear_part_ld((int)L->n_out, L->gated != 0);
+      if (align_up(bytes) > need) need = align_up(bytes);
+    }
+  }
+  return need;
+}
+
+}  // namespace
+
+extern "C" {
+
+exfold_status exfold_route_experts(const exfold_routing *r, const void *logits, int32_t dtype,
+                                   int64_t ld, int64_t T, int64_t N, int64_t K, int32_t *topk_ids,
+                                   float *topk_w, void *stream) {
+  if (!r) return EXFOLD_ERR_NULL;
+  if (dtype != EXFOLD_F32 && dtype != EXFOLD_BF16) return EXFOLD_ERR_DTYPE;
+  exfold_status st = check_routing(T, N, K);
+  if (st != EXFOLD_OK) return st;
+  if (r->score != EXFOLD_SCORE_SOFTMAX && r->score != EXFOLD_SCORE_SIGMOID) return EXFOLD_ERR_ARG;
+  if (r->group_value != EXFOLD_GROUP_MAX && r->group_value != EXFOLD_GROUP_TOP2) return EXFOLD_ERR_ARG;
+  if (!(r->scale > 0.f && r->scale <= 3.402823466e+38f)) return EXFOLD_ERR_ARG;
+  if (r->n_groups < 1 || r->n_groups > N || N % r->n_groups != 0) return EXFOLD_ERR_SHAPE;
+  if (r->keep_groups < 1 || r->keep_groups > r->n_groups || r->keep_groups * (N / r->n_groups) < K)
+    return EXFOLD_ERR_SHAPE;
+  if (ld < N || ld > kMaxStride) return EXFOLD_ERR_SHAPE;
+  if (T == 0) return EXFOLD_OK;
+  if (!logits || !topk_ids || !topk_w) return EXFOLD_ERR_NULL;
+  if (unaligned_to(logits, element(dtype)) || unaligned_to(topk_ids, 4) || unaligned_to(topk_w, 4) ||
+      unaligned_to(r->select_bias, 4))
+    return EXFOLD_ERR_ALIGN;
+  const Extent ei = extent(topk_ids, 1, T * K, T * K, 4), ew = extent(topk_w, 1, T * K, T * K, 4),
+               el = extent(logits, T, ld, N, (int64_t)element(dtype)), eb = extent(r->select_bias, 1, N, N, 4);
+  if (overlap(ei, ew) || overlap(ei, el) || overlap(ew, el) || overlap(ei, eb) || overlap(ew, eb)) return EXFOLD_ERR_ARG;
+  RouteExpertsArgs a{};
+  a.logits = logits;
+  a.dtype = dtype;
+  a.ld = ld;
+  a.T = (int)T;
+  a.N = (int)N;
+  a.K = (int)K;
+  a.n_groups = (int)r->n_groups;
+  a.keep_groups = (int)r->keep_groups;
+  a.score = r->score;
+  a.group_value = r->group_value;
+  a.renorm = r->renorm != 0;
+  a.scale = r->scale;
+  a.bias = r->select_bias;
+  a.ids = topk_ids;
+  a.w = topk_w;
+  return launch_route_experts(a, static_cast<hipStream_t>(stream)) == hipSuccess ? EXFOLD_OK : EXFOLD_ERR_DEVICE;
+}
+
+size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M) {
+  return check_linear(linear, M) == EXFOLD_OK ? linear_need(linear, M) : 0;
+}
+
+exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64_t ldx, int64_t M,
+                                    const void *residual, int64_t ldr, void *y, int64_t ldy, void *ws,
+                                    size_t ws_bytes, void *stream) {
+  exfold_status st = check_linear(L, M);
+  if (st != EXFOLD_OK) return st;
+  if (ldx < L->n_in || ldx > kMaxStride || ldy < L->n_out || ldy > kMaxStride) return EXFOLD_ERR_SHAPE;
+  if (residual && (ldr < L->n_out || ldr > kMaxStride)) return EXFOLD_ERR_SHAPE;
+  if (M == 0) return EXFOLD_OK;
+  if (!x || !y) return EXFOLD_ERR_NULL;
+  const int64_t esz = (int64_t)element(L->dtype), osz = (int64_t)element(L->out_dtype);
+  if (unaligned_to(x, esz) || unaligned_to(y, osz) || unaligned_to(residual, osz)) return EXFOLD_ERR_ALIGN;
+  const size_t need = linear_need(L, M);
+  st = check_ws(ws, ws_bytes, need);
+  if (st != EXFOLD_OK) return st;
+  const int64_t rows_w = L->n_out * (L->gated ? 2 : 1);
+  const Extent ey = extent(y, M, ldy, L->n_out, osz), ex = extent(x, M, ldx, L->n_in, esz),
+               ew = extent(L->w, rows_w, L->ldw, L->n_in, esz), eb = extent(L->bias, 1, rows_w, rows_w, 4),
+               er = extent(residual, M, ldr, L->n_out, osz), es{reinterpret_cast<uintptr_t>(ws), 1, (int64_t)need, (int64_t)need};
+  const bool in_place = residual == y && (ldr == ldy || M == 1);
+  if (overlap(ey, ex) || overlap(ey, ew) || overlap(ey, eb) || (!in_place && overlap(ey, er))) return EXFOLD_ERR_ARG;
+  if (overlap(es, ey) || overlap(es, ex) || overlap(es, ew) || overlap(es, eb) || overlap(es, er)) return EXFOLD_ERR_ARG;
+  LinearArgs a{};
+  a.x = x;
+  a.w = L->w;
+  a.bias = L->bias;
+  a.res = residual;
+  a.y = y;
+  a.ldx = ldx;
+  a.ldw = L->ldw;
+  a.ldr = residual ? ldr : 0;
+  a.ldy = ldy;
+  a.M = (int)M;
+  a.N = (int)L->n_out;
+  a.K = (int)L->n_in;
+  a.dtype = L->dtype;
+  a.out_dtype = L->out_dtype;
+  a.act = L->act;
+  a.gated = L->gated != 0;
+  a.part = static_cast<float *>(ws);
+  const bool vec = !misaligned(x) && !misaligned(L->w) && ldx * esz % 16 == 0 && L->ldw * esz % 16 == 0 && L->n_in * esz % 16 == 0;
+  const LinearPlan p = plan_linear(a.dtype, a.gated, vec, a.M, a.N, a.K, cu_count());
+  return launch_linear(a, p, vec, static_cast<hipStream_t>(stream)) == hipSuccess ? EXFOLD_OK : EXFOLD_ERR_DEVICE;
+}
+
+}  // extern "C"

@@ -39,6 +39,44 @@ hipError_t launch_decode_pool_fold(const int32_t *ids, const float *w, int B, in
                                    int32_t *pool, int32_t *pool_size, int32_t *out_ids,
                                    float *out_w, int32_t *tgt, float *scl, hipStream_t s);
 
+// ---- routing of tokens to experts from logits (k_score.hip) ----
+struct RouteExpertsArgs {
+  const void *logits;  // [T, N] float32 or bf16, rows ld elements apart
+  int dtype;
+  long long ld;
+  int T, N, K, n_groups, keep_groups, score, group_value, renorm;
+  float scale;
+  const float *bias;  // [N] selection bias, or nullptr
+  int32_t *ids;       // [T, K]
+  float *w;           // [T, K]
+};
+hipError_t launch_route_experts(const RouteExpertsArgs &a, hipStream_t s);
+
+// ---- matrix product with an epilogue (k_linear.hip) ----
+struct LinearArgs {
+  const void *x, *w;  // [M, K], [N or (gated) 2N, K]
+  const float *bias;  // [N or 2N], or nullptr
+  const void *res;    // [M, N] in y's type, or nullptr
+  void *y;            // [M, N]
+  long long ldx, ldw, ldr, ldy;
+  int M, N, K, dtype, out_dtype, act;
+  bool gated;
+  float *part;  // [ksplit][M][linear_part_ld] float32 partial sums, when split
+};
+// Kernel families of the product.
+enum { kLinTile = 0 };
+struct LinearPlan {
+  int kind;
+  int bm, bn;  // tile rows, and weight rows of a tile
+  int ksplit;  // splits of the reduction, joined by a second kernel
+  int kc;      // columns of a split (the last may hold fewer)
+  int grid;
+};
+// vec: rows of x and w start on 16 bytes and K is a whole number of 16-byte pieces.
+LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int cu_count);
+__host__ __device__ inline long long linear_part_ld(int N, bool gated) { return ((long long)N * (gated ? 2 : 1) + 3) / 4 * 4; }
+hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, bool vec, hipStream_t s);
+
 // ---- permutation (k_permute.hip) ----
 constexpr int kPermSlotsPerBlock = 1024;
 struct PermBuffers {

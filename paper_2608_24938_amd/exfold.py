@@ -23,6 +23,8 @@ SCRATCH_BYTES = 64 << 20   # EXFOLD_SCRATCH_BYTES
 F32, BF16 = 0, 1
 PHASE = {"dense": 0, "prefill": 1, "decode": 2, "decode_static": 3, "prefill_diag": 4}
 CAL_MODE = {"corouted": 0, "common": 1}
+SCORE = {"softmax": 0, "sigmoid": 1}
+ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 
 EXPORTED = [
     "exfold_select_prefill", "exfold_select_decode_pool", "exfold_fold_gates", "exfold_static_pool",
@@ -31,6 +33,7 @@ EXPORTED = [
     "exfold_moe_execute", "exfold_calibrate_workspace_size", "exfold_calibrate_projectors",
     "exfold_calibrate_diagonal",
     "exfold_status_str", "exfold_gemm_plan",
+    "exfold_route_experts", "exfold_linear_workspace_size", "exfold_linear_forward",
 ]
 
 
@@ -52,6 +55,18 @@ class _Tables(ctypes.Structure):
     _fields_ = [("S", ctypes.c_void_p), ("L", ctypes.c_void_p), ("h", ctypes.c_void_p),
                 ("tgt", ctypes.c_void_p), ("scl", ctypes.c_void_p), ("loss_cap", ctypes.c_float),
                 ("fold_flags", ctypes.c_int32), ("Dg", ctypes.c_void_p)]
+
+
+class _Routing(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("group_value", ctypes.c_int32), ("n_groups", ctypes.c_int64),
+                ("keep_groups", ctypes.c_int64), ("renorm", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("select_bias", ctypes.c_void_p)]
+
+
+class _Linear(ctypes.Structure):
+    _fields_ = [("n_in", ctypes.c_int64), ("n_out", ctypes.c_int64), ("ldw", ctypes.c_int64), ("w", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("gated", ctypes.c_int32)]
 
 
 FOLD_LOSS_CAP, FOLD_RENORM, FOLD_CONFIDENCE = 1, 2, 4
@@ -101,6 +116,9 @@ def lib() -> ctypes.CDLL:
             "exfold_calibrate_diagonal": (i32, [vp, vp, i64, dbl, i32, vp, vp, vp, sz, vp]),
             "exfold_status_str": (ctypes.c_char_p, [i32]),
             "exfold_gemm_plan": (i32, [vp, i64, i64, i32, vp]),
+            "exfold_route_experts": (i32, [vp, vp, i32, i64, i64, i64, i64, vp, vp, vp]),
+            "exfold_linear_workspace_size": (sz, [vp, i64]),
+            "exfold_linear_forward": (i32, [vp, vp, i64, i64, vp, i64, vp, i64, vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -386,3 +404,119 @@ def calibrate_diagonal(layer: Layer, x_cal, lam: float = 1e-3, mode: str = "coro
     _check(lib().exfold_calibrate_diagonal(ctypes.byref(ls), _ptr(x_cal), m, lam, CAL_MODE[mode], _ptr(Dg), _ptr(Ld),
                                            _ptr(ws), ws.numel(), _stream(stream)), "exfold_calibrate_diagonal")
     return Dg, Ld
+
+
+_DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _matrix(t, name, dtype=None, shape=None, device=None):
+    """Row stride of a 2-D GPU tensor whose rows are contiguous (gaps between rows allowed)."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in _DTYPE or (t.shape[1] > 1 and t.stride(1) != 1) \
+            or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != shape) \
+            or (device is not None and t.device != device):
+        raise ValueError(f"{name}: expected a 2-D {dtype or 'float32 or bfloat16'} tensor"
+                         f"{'' if shape is None else f' {shape}'} with contiguous rows on "
+                         f"{'the GPU' if device is None else device}, got {t.dtype} {tuple(t.shape)} with strides "
+                         f"{t.stride()} on {t.device}")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t, n, name, device):
+    if t is not None and (t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous() or t.device != device):
+        raise ValueError(f"{name}: expected contiguous float32 ({n},) on {device}, got {t.dtype} {tuple(t.shape)} "
+                         f"on {t.device}")
+
+
+def _call_on(device, stream, where, fn, *args):
+    """fn(*args, stream) on the tensors' device: the given stream, or that device's current one."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"{where}: the stream is on {stream.device}, the tensors on {device}")
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(stream)), where)
+        return
+    with torch.cuda.device(device):
+        _check(fn(*args, _stream(stream)), where)
+
+
+def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, keep_groups=1, group_top2=False,
+                  renorm=True, scale=1.0, topk_ids=None, topk_w=None, stream=None):
+    """Routes of every token from its router logits [T, N] (float32 or bfloat16): (ids [T, K] int32, w [T, K] float32).
+
+    score: "softmax" or "sigmoid" over all experts.  select_bias: [N] float32 added to the scores for the
+    selection only.  groups, keep_groups: the selection is limited to the keep_groups of `groups` groups of
+    consecutive experts with the largest value (their largest expert, or group_top2: the sum of the two
+    largest).  renorm: the weights of a token's routes are divided by their sum; scale multiplies them.
+    A logit of -inf masks its expert (see exfold_routing in the header).  topk_ids/topk_w: optional outputs."""
+    ld = _matrix(logits, "logits")
+    T, N = logits.shape
+    dev = logits.device
+    _vector(select_bias, N, "select_bias", dev)
+    if score not in SCORE:
+        raise ValueError(f"score: expected one of {sorted(SCORE)}, got {score!r}")
+    if topk_ids is None:
+        topk_ids = torch.empty((T, top_k), dtype=torch.int32, device=dev)
+    else:
+        _need(topk_ids, torch.int32, (T, top_k), "topk_ids")
+    if topk_w is None:
+        topk_w = torch.empty((T, top_k), dtype=torch.float32, device=dev)
+    else:
+        _need(topk_w, torch.float32, (T, top_k), "topk_w")
+    if topk_ids.device != dev or topk_w.device != dev:
+        raise ValueError(f"topk_ids, topk_w: expected on {dev}")
+    r = _Routing(SCORE[score], 1 if group_top2 else 0, groups, keep_groups, 1 if renorm else 0, scale,
+                 None if select_bias is None else select_bias.data_ptr())
+    _call_on(dev, stream, "exfold_route_experts", lib().exfold_route_experts, ctypes.byref(r), logits.data_ptr(),
+             _DTYPE[logits.dtype], ld, T, N, top_k, topk_ids.data_ptr(), topk_w.data_ptr())
+    return topk_ids, topk_w
+
+
+def _linear_struct(w, ldw, n_out, bias, act, gated, out_dtype):
+    if act not in ACT:
+        raise ValueError(f"act: expected one of {sorted(ACT)}, got {act!r}")
+    if out_dtype not in _DTYPE:
+        raise ValueError(f"out_dtype: expected float32 or bfloat16, got {out_dtype}")
+    return _Linear(w.shape[1], n_out, ldw, w.data_ptr(), None if bias is None else bias.data_ptr(), _DTYPE[w.dtype],
+                   _DTYPE[out_dtype], ACT[act], 1 if gated else 0)
+
+
+def linear_workspace_size(w, rows, gated=False) -> int:
+    """Bytes of workspace of linear() for `rows` rows of x and this weight."""
+    n_out = w.shape[0] // 2 if gated else w.shape[0]
+    ls = _linear_struct(w, _matrix(w, "w"), n_out, None, "none", gated, w.dtype)
+    n = lib().exfold_linear_workspace_size(ctypes.byref(ls), rows)
+    if n == 0:
+        raise ValueError("invalid shape for exfold_linear_forward")
+    return n
+
+
+def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=None, y=None, workspace=None, stream=None):
+    """y = act(x w^T + bias) + residual; gated: y = act(x w_g^T + b_g) * (x w_u^T + b_u) + residual.
+
+    x [M, n_in] and w [n_out, n_in] (gated: [2 n_out, n_in], gate rows first) of one type, float32 or
+    bfloat16, rows contiguous; bias [n_out] (gated [2 n_out]) float32; residual and y [M, n_out] of
+    out_dtype (x's type unless given; float32 is always allowed).  y may be the residual (y += ...).
+    act: "none", "relu", "silu", "gelu" or "gelu_tanh".  workspace: linear_workspace_size bytes, made here
+    unless given."""
+    ldx = _matrix(x, "x")
+    dev = x.device
+    M, K = x.shape
+    rows = w.shape[0] if w.dim() == 2 else 0
+    if gated and rows % 2:
+        raise ValueError(f"w: a gated product has as many gate as up rows, got {rows} rows")
+    ldw = _matrix(w, "w", x.dtype, (rows, K), dev)
+    n_out = rows // 2 if gated else rows
+    _vector(bias, rows, "bias", dev)
+    if out_dtype is None:
+        out_dtype = x.dtype if y is None else y.dtype
+    ldr = 0 if residual is None else _matrix(residual, "residual", out_dtype, (M, n_out), dev)
+    if y is None:
+        y = torch.empty((M, n_out), dtype=out_dtype, device=dev)
+    ldy = _matrix(y, "y", out_dtype, (M, n_out), dev)
+    ls = _linear_struct(w, ldw, n_out, bias, act, gated, out_dtype)
+    p = ctypes.byref(ls)
+    if workspace is None:
+        workspace = _workspace(lib().exfold_linear_workspace_size(p, M), dev, stream)
+    _call_on(dev, stream, "exfold_linear_forward", lib().exfold_linear_forward, p, x.data_ptr(), ldx, M,
+             None if residual is None else residual.data_ptr(), ldr, y.data_ptr(), ldy, workspace.data_ptr(),
+             workspace.numel() * workspace.element_size())
+    return y

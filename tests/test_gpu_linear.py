@@ -1,0 +1,281 @@
+"""exfold_linear_forward against its float64 definition, element by element.
+
+Tolerances are derived: a float32 sum of K products and a bias is off by at most
+gamma = (K + 2) 2^-24 of the sum of magnitudes, in any order; the activations have slopes
+below 1.13 (gated products: the product rule) and are evaluated within 16 float32 roundings
+of |z| (z sigmoid(u): an error of |u| 2^-23 in the exponent is damped by the sigmoid's own
+tail, 1 + erf by nothing); the residual is one more float32 rounding, the output half a step
+of its type (bf16 2^-8, float32 2^-24)."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import exfold_oracle as O
+from oracle import operators_oracle as P
+from paper_2608_24938_amd import exfold as X
+from paper_2608_24938_amd import synth
+
+from .gpu_common import DEV, LayerPair, from_dev, per_token_rel_l2, sync, to_dev
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+HALF = {torch.float32: U32, torch.bfloat16: 2.0 ** -8}
+
+
+def bound(K, z, mag, ref, act, gated, residual, out_dtype):
+    dz = (K + 2) * U32 * mag
+    slope, ev = (1.0, 0.0) if act == "none" else (1.13, 16 * U32)
+    n = z.shape[1] // 2 if gated else z.shape[1]
+    a = P.activate(act, z[:, :n])
+    da = slope * dz[:, :n] + ev * np.abs(z[:, :n])
+    if gated:
+        da = da * (np.abs(z[:, n:]) + dz[:, n:]) + np.abs(a) * dz[:, n:] + U32 * np.abs(a * z[:, n:])
+    res = 0.0 if residual is None else np.abs(residual)
+    before = da + U32 * (np.abs(ref) + res)
+    return before + (HALF[out_dtype] + U32) * (np.abs(ref) + before) + 2.0 ** -126
+
+
+def data(M, N, K, dtype, gated, bias, residual, out_dtype, seed=0, pad=0, wpad=0):
+    g = torch.Generator().manual_seed(seed + M * 7 + N * 3 + K)
+    rows = 2 * N if gated else N
+    x = torch.randn(M, K + pad, generator=g).to(dtype).to(DEV)[:, :K]
+    w = (torch.randn(rows, K + wpad, generator=g) * (1.5 / K ** 0.5)).to(dtype).to(DEV)[:, :K]
+    b = torch.randn(rows, generator=g).to(DEV) if bias else None
+    r = torch.randn(M, N, generator=g).to(out_dtype).to(DEV) if residual else None
+    return x, w, b, r
+
+
+def np64(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def compare(y, x, w, b, r, act, gated):
+    ref, z, mag = P.linear(np64(x), np64(w), np64(b), act, gated, np64(r))
+    lim = bound(x.shape[1], z, mag, ref, act, gated, np64(r), y.dtype)
+    err = np.abs(np64(y) - ref)
+    assert np.isfinite(np64(y)).all()
+    worst = np.unravel_index(np.argmax(err / lim), err.shape)
+    assert (err <= lim).all(), f"at {worst}: {np64(y)[worst]} against {ref[worst]}, limit {lim[worst]}"
+
+
+SIZES = [(1, 1, 1), (1, 128, 2048), (1, 7, 13), (2, 100, 64), (3, 33, 515), (4, 256, 1000), (5, 64, 128), (8, 129, 72),
+         (9, 40, 4096), (16, 1000, 256), (17, 65, 320), (31, 96, 2056), (33, 512, 64), (48, 130, 1003), (64, 384, 768),
+         (65, 31, 8), (100, 300, 192), (129, 128, 100), (200, 257, 1408), (300, 140, 333)]
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype,out_dtype", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32),
+                                             (torch.float32, torch.float32)])
+def test_sizes(M, N, K, gated, dtype, out_dtype):
+    act = ("none", "relu", "silu", "gelu", "gelu_tanh")[(M + N + K) % 5]
+    for bias, residual in ((False, False), (True, True)):
+        x, w, b, r = data(M, N, K, dtype, gated, bias, residual, out_dtype)
+        y = X.linear(x, w, bias=b, act=act, gated=gated, residual=r, out_dtype=out_dtype)
+        sync()
+        assert y.dtype == out_dtype and y.shape == (M, N)
+        compare(y, x, w, b, r, act, gated)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("M", [2, 24, 150])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_activations_over_their_range(act, M, dtype):
+    # sums from about -60 to 60: the tails of every activation
+    x, w, b, r = data(M, 90, 64, dtype, True, True, True, dtype, seed=4)
+    x = (x * torch.linspace(0.1, 30, M, device=DEV)[:, None]).to(dtype)
+    for gated in (False, True):
+        wg, bg = (w, b) if gated else (w[:90], b[:90])
+        compare(X.linear(x, wg, bias=bg, act=act, gated=gated, residual=r), x, wg, bg, r, act, gated)
+
+
+# row counts around the borders of the tiles, with long reductions (split) and short ones
+@pytest.mark.parametrize("M,N,K,gated,dtype,out_dtype", [
+    (1, 4096, 1408, False, torch.bfloat16, torch.bfloat16), (2, 1408, 4096, True, torch.bfloat16, torch.bfloat16),
+    (16, 64, 14336, False, torch.bfloat16, torch.float32), (32, 256, 14336, False, torch.bfloat16, torch.bfloat16),
+    (64, 128, 8192, True, torch.bfloat16, torch.bfloat16), (128, 256, 4096, False, torch.bfloat16, torch.float32),
+    (255, 512, 2048, False, torch.bfloat16, torch.bfloat16), (256, 1000, 1024, True, torch.bfloat16, torch.bfloat16),
+    (1237, 1408, 512, True, torch.bfloat16, torch.bfloat16), (1500, 768, 2048, False, torch.bfloat16, torch.bfloat16),
+    (2049, 2050, 256, False, torch.bfloat16, torch.bfloat16), (1111, 700, 129, True, torch.bfloat16, torch.bfloat16),
+    (3, 600, 4100, False, torch.float32, torch.float32), (700, 515, 768, False, torch.float32, torch.float32),
+    (2000, 256, 260, True, torch.float32, torch.float32), (40, 64, 9000, False, torch.float32, torch.float32),
+])
+def test_large(M, N, K, gated, dtype, out_dtype):
+    x, w, b, r = data(M, N, K, dtype, gated, True, True, out_dtype)
+    compare(X.linear(x, w, bias=b, act="silu", gated=gated, residual=r, out_dtype=out_dtype), x, w, b, r, "silu", gated)
+
+
+@pytest.mark.parametrize("M,N,K,gated", [(1, 40, 64, False), (6, 100, 128, True), (20, 72, 200, False),
+                                         (70, 130, 192, True), (200, 256, 256, False), (600, 300, 128, False)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("pad,shift", [(64, 0), (8, 8), (5, 3), (0, 1)])
+def test_strides_alignment_and_what_lies_between(M, N, K, gated, dtype, pad, shift):
+    # x, w, the residual and y are slices of wider buffers, `shift` elements in; y's buffer keeps the rest
+    rows = 2 * N if gated else N
+    g = torch.Generator().manual_seed(M + pad)
+    cut = lambda rr, cc, scale=1.0: (torch.randn(rr * (cc + pad) + shift, generator=g) * scale).to(dtype).to(DEV)[shift:] \
+        .view(rr, cc + pad)[:, :cc]                                                     # noqa: E731
+    x, w, r = cut(M, K), cut(rows, K, 1.5 / K ** 0.5), cut(M, N)
+    ybuf = torch.full((M * (N + pad) + shift + 7,), 7.0, dtype=dtype, device=DEV)
+    y = ybuf[shift:shift + M * (N + pad)].view(M, N + pad)[:, :N]
+    out = X.linear(x, w, act="gelu", gated=gated, residual=r, y=y)
+    sync()
+    assert out.data_ptr() == y.data_ptr()
+    compare(y, x, w, None, r, "gelu", gated)
+    mark = ybuf.clone()
+    mark[shift:shift + M * (N + pad)].view(M, N + pad)[:, :N] = 7.0
+    assert (mark == 7.0).all()                                                          # nothing beside y's rows
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 256, 512), (12, 129, 2048), (100, 128, 4096), (1024, 512, 128)])
+def test_adds_onto_its_residual_in_place(M, N, K):
+    for dtype in (torch.bfloat16, torch.float32):
+        x, w, b, r = data(M, N, K, dtype, False, True, True, dtype)
+        y = r.clone()
+        X.linear(x, w, bias=b, residual=y, y=y)
+        compare(y, x, w, b, r, "none", False)
+
+
+def test_column_slices_of_one_buffer():
+    # x and y are column ranges of one buffer: no overlap, and allowed
+    buf = torch.randn(50, 96 + 64, generator=torch.Generator().manual_seed(0)).bfloat16().to(DEV)
+    w = (0.1 * torch.randn(64, 96, generator=torch.Generator().manual_seed(1))).bfloat16().to(DEV)
+    x = buf[:, :96].clone()
+    X.linear(buf[:, :96], w, y=buf[:, 96:])
+    sync()
+    assert torch.equal(buf[:, :96], x)
+    compare(buf[:, 96:], x, w, None, None, "none", False)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 300, 1024), (24, 300, 4096), (90, 128, 4096), (513, 640, 512)])
+def test_infinities_and_nan_stay_in_their_rows(M, N, K):
+    # a row of x holding NaN or infinities says nothing about the others (padding rows, masked tokens)
+    x, w, b, r = data(M + 2, N, K, torch.bfloat16, False, True, True, torch.bfloat16)
+    x[0], x[-1, 3] = float("nan"), float("inf")
+    y = X.linear(x, w, bias=b, act="silu", residual=r)
+    sync()
+    assert y[0].isnan().all()
+    compare(y[1:-1], x[1:-1], w, b, r[1:-1], "silu", False)
+
+
+@pytest.mark.parametrize("M,N,K,gated", [(1, 1408, 4096, True), (32, 512, 14336, False), (200, 256, 4096, False),
+                                         (1024, 512, 1024, True)])
+def test_identical_calls_and_graph_replays_are_bitwise_equal(M, N, K, gated):
+    x, w, b, r = data(M, N, K, torch.bfloat16, gated, True, True, torch.bfloat16)
+    y = torch.empty_like(r)
+    ws = torch.empty(X.linear_workspace_size(w, M, gated), dtype=torch.uint8, device=DEV)
+
+    def call(out, work):
+        X.linear(x, w, bias=b, act="silu", gated=gated, residual=r, y=out, workspace=work)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(y, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    sync()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(y, ws)
+    for rep in range(4):
+        x.copy_(torch.randn(M, K, generator=torch.Generator().manual_seed(rep)).bfloat16())
+        ref = torch.empty_like(y)
+        call(ref, None)
+        again = torch.empty_like(y)
+        call(again, None)
+        ws.fill_(0xFF)                                  # nothing is kept in the workspace between calls
+        y.zero_()
+        graph.replay()
+        sync()
+        assert torch.equal(ref.view(torch.int16), again.view(torch.int16))
+        assert torch.equal(ref.view(torch.int16), y.view(torch.int16)), f"replay {rep}"
+
+
+def test_calls_on_two_streams():
+    a = data(64, 128, 8192, torch.bfloat16, False, True, False, torch.bfloat16)
+    c = data(64, 128, 8192, torch.bfloat16, False, True, False, torch.bfloat16, seed=9)
+    sync()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = [(X.linear(*a[:2], bias=a[2], stream=s1), X.linear(*c[:2], bias=c[2], stream=s2)) for _ in range(5)]
+    sync()
+    for y1, y2 in outs:
+        compare(y1, *a, "none", False)
+        compare(y2, *c, "none", False)
+
+
+def test_empty_batch_and_binding_refusals():
+    w = torch.zeros(6, 8, device=DEV, dtype=torch.bfloat16)
+    x = torch.zeros(4, 8, device=DEV, dtype=torch.bfloat16)
+    assert X.linear(x[:0], w).shape == (0, 6)
+    for bad in (dict(act="tanh"), dict(bias=torch.zeros(5, device=DEV)), dict(bias=torch.zeros(6)),
+                dict(residual=torch.zeros(4, 5, device=DEV, dtype=torch.bfloat16)),
+                dict(residual=torch.zeros(4, 6, device=DEV)), dict(out_dtype=torch.float16),
+                dict(y=torch.zeros(4, 6, device=DEV), out_dtype=torch.bfloat16)):
+        with pytest.raises(ValueError):
+            X.linear(x, w, **bad)
+    for xb, wb in ((x.float(), w), (x[:, :7], w), (x.t(), w), (x[0], w), (x, w[0]), (x, w.t())):
+        with pytest.raises(ValueError):
+            X.linear(xb, wb)
+    with pytest.raises(ValueError):
+        X.linear(x, w[:5], gated=True)
+    with pytest.raises(X.ExfoldError):
+        X.linear(x.float(), w.float(), out_dtype=torch.bfloat16)
+    with pytest.raises(X.ExfoldError):
+        X.linear(x, w, workspace=torch.empty(255, dtype=torch.uint8, device=DEV))
+    with pytest.raises(X.ExfoldError):
+        X.linear(x, w, y=torch.zeros(1, 6, device=DEV, dtype=torch.bfloat16).expand(4, 6))
+
+
+BLOCK = synth.LayerShape("block", d=512, inter=256, n_experts=64, top_k=6, dtype="bf16", router_bias=True)
+
+
+@pytest.mark.parametrize("T,phase,budget", [(1, "decode", 8), (40, "decode", 16), (300, "prefill", 3), (300, "dense", 0)])
+def test_block_of_linear_routing_folding_and_experts(T, phase, budget):
+    """A layer with sigmoid routing and a shared expert of another width than the routed ones, as a user
+    composes it: router logits, routes, selection and fold, routed experts, shared expert added in place."""
+    lp = LayerPair(BLOCK, seed=7)
+    N, K, Is = BLOCK.n_experts, BLOCK.top_k, 320
+    S, L, h = (to_dev(a) for a in synth.synthetic_tables(N, seed=7))
+    x = to_dev(synth.tokens(BLOCK, T, seed=7))
+    g = torch.Generator().manual_seed(7)
+    sgu = (0.02 * torch.randn(2 * Is, 512, generator=g)).bfloat16().to(DEV)
+    sdn = (0.02 * torch.randn(512, Is, generator=g)).bfloat16().to(DEV)
+    balance = (0.05 * torch.randn(N, generator=g)).to(DEV)
+
+    logits = X.linear(x, lp.dev.w_router, bias=lp.dev.router_bias, out_dtype=torch.float32)
+    ids, w = X.route_experts(logits, K, score="sigmoid", select_bias=balance, groups=8, keep_groups=4,
+                             group_top2=True, scale=2.5)
+    out_ids, out_w = ids, w
+    if phase == "prefill":
+        _, _, keep = X.select_prefill(h, budget, topk_ids=ids, topk_w=w)
+        out_ids, out_w = X.fold_gates("prefill", budget, ids, w, S, L, keep=keep)
+    elif phase == "decode":
+        _, _, pool, size = X.select_decode_pool(h, budget, topk_ids=ids, topk_w=w)
+        out_ids, out_w = X.fold_gates("decode", budget, ids, w, S, L, pool=pool, pool_size=size)
+    y = X.moe_execute(lp.dev, x, out_ids, out_w)
+    routed = y.clone()
+    hid = X.linear(x, sgu, act="silu", gated=True)
+    X.linear(hid, sdn, residual=y, y=y)
+    sync()
+
+    xf = from_dev(x).astype(np.float64)
+    compare(logits, x, lp.dev.w_router, lp.dev.router_bias, None, "none", False)
+    rid, rw = P.route_experts(logits.cpu().numpy(), K, score="sigmoid", select_bias=balance.cpu().numpy(), groups=8,
+                              keep_groups=4, group_top2=True, scale=2.5)
+    np.testing.assert_array_equal(ids.cpu().numpy(), rid)
+    wf = w.cpu().numpy()
+    np.testing.assert_allclose(wf, rw, rtol=2.0 ** -23)
+    Sn, Ln, hn = (a.cpu().numpy() for a in (S, L, h))
+    ref_ids, ref_w = rid, wf
+    if phase == "prefill":
+        ref_ids, ref_w = O.fold_prefill(rid, wf, O.select_prefill(rid, wf, hn, budget), Sn, Ln)[:2]
+    elif phase == "decode":
+        ref_ids, ref_w = O.fold_decode(rid, wf, O.select_decode_pool(rid, wf, hn, N, budget)[0], Sn, Ln, N)[:2]
+    np.testing.assert_array_equal(out_ids.cpu().numpy(), ref_ids)
+    np.testing.assert_array_equal(out_w.cpu().numpy(), np.asarray(ref_w, dtype=np.float32))
+    ref = O.moe_output(lp.ref, xf, ref_ids, np.asarray(ref_w, dtype=np.float64))
+    assert per_token_rel_l2(from_dev(routed), ref).max() <= 2e-2
+    compare(hid, x, sgu, None, None, "silu", True)
+    compare(y, hid, sdn, None, routed, "none", False)
