@@ -458,9 +458,9 @@ typedef struct exfold_linear {
   int32_t gated;      /* 0 or 1                                                    */
 } exfold_linear;
 
-/* Bytes of workspace exfold_linear_forward needs for M rows (at least 256), or 0 on
- * invalid input.  Needed for its partial sums only, so calls that overlap in time (other
- * streams, graphs replayed together) need workspaces of their own. */
+/* Bytes of workspace exfold_linear_forward needs for M rows: 0 where it needs none (ws may
+ * then be NULL), and on invalid input.  It holds partial sums during the call, so calls that
+ * overlap in time (other streams, graphs replayed together) need workspaces of their own. */
 size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M);
 
 /*

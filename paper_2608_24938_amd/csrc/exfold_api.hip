@@ -797,7 +797,7 @@ exfold_status check_linear(const exfold_linear *L, int64_t M) {
 }
 
 size_t linear_need(const exfold_linear *L, int64_t M) {
-  size_t need = kAlign;
+  size_t need = 0;
   for (int vec = 0; vec < 2; ++vec) {  // what the pointers and strides of the call allow
     const LinearPlan p = plan_linear(L->dtype, L->gated != 0, vec != 0, (int)M, (int)L->n_out, (int)L->n_in, cu_count());
     if (p.ksplit > 1) {
@@ -869,12 +869,14 @@ exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64
   const int64_t esz = (int64_t)element(L->dtype), osz = (int64_t)element(L->out_dtype);
   if (unaligned_to(x, esz) || unaligned_to(y, osz) || unaligned_to(residual, osz)) return EXFOLD_ERR_ALIGN;
   const size_t need = linear_need(L, M);
-  st = check_ws(ws, ws_bytes, need);
-  if (st != EXFOLD_OK) return st;
+  if (need > 0) {
+    st = check_ws(ws, ws_bytes, need);
+    if (st != EXFOLD_OK) return st;
+  }
   const int64_t rows_w = L->n_out * (L->gated ? 2 : 1);
   const Extent ey = extent(y, M, ldy, L->n_out, osz), ex = extent(x, M, ldx, L->n_in, esz),
                ew = extent(L->w, rows_w, L->ldw, L->n_in, esz), eb = extent(L->bias, 1, rows_w, rows_w, 4),
-               er = extent(residual, M, ldr, L->n_out, osz), es{reinterpret_cast<uintptr_t>(ws), 1, (int64_t)need, (int64_t)need};
+               er = extent(residual, M, ldr, L->n_out, osz), es{need > 0 ? reinterpret_cast<uintptr_t>(ws) : 0, 1, (int64_t)need, (int64_t)need};
   const bool in_place = residual == y && (ldr == ldy || M == 1);
   if (overlap(ey, ex) || overlap(ey, ew) || overlap(ey, eb) || (!in_place && overlap(ey, er))) return EXFOLD_ERR_ARG;
   if (overlap(es, ey) || overlap(es, ex) || overlap(es, ew) || overlap(es, eb) || overlap(es, er)) return EXFOLD_ERR_ARG;

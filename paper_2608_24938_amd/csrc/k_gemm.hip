@@ -18,6 +18,7 @@
 // combine adds the splits in a fixed order.
 #include "common.hpp"
 #include "kernels.hpp"
+#include "linear_epilogue.hpp"
 
 namespace exfold {
 
@@ -467,18 +468,19 @@ constexpr int kWideSmemElems = 2 * (kWide / 2 + 2 * kWideBN) * kWideBK;
 // groups gain most, in their tail tiles (8192 Qwen3-shaped tokens, K' = 4: 247 ->
 // 229 and 177 -> 156 us; pipes busy 47.5 -> 52% and 36 -> 40%).
 //
+// row_a(r): start of the tile's row r of the first operand; row_b(g, r): start of row r of
+// weight half g.  Rows past the operand's end may be any valid row: they are not stored.
+//
 // TMV: 32-row blocks of the wave that hold rows of the group (full: 2 .. 4, tail:
 // 0 .. 2; the others' fragments are not read and their MFMAs not issued).
-template <bool GATE_UP, bool DBL, int TMV>
-__device__ __forceinline__ void wide_tile_mma(const GemmKArgs &p, const TileId &t, int row0, int valid,
-                                              int k0, int k1, bf16_t *smem,
+template <bool DBL, int TMV, typename RowA, typename RowB>
+__device__ __forceinline__ void wide_tile_mma(const RowA &row_a, const RowB &row_b, int k0, int k1, bf16_t *smem,
                                               f32x16 (&acc)[kWideTM][kWideTN]) {
   constexpr int HALF = 128 * kWideBK;             // elements of a half tile
   constexpr int NA = DBL ? 1 : 2, NB = DBL ? 4 : 2;  // half tiles of a stage
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  const bf16_t *Wg = (t.g < p.n_experts) ? p.W + (long long)t.g * p.w_stride : p.Ws;
   // Wave w fills 1 KiB blocks w and w + 8 of a half tile: rows 8 w .. + 7 and 64
   // further, lane l the chunk that the swizzle puts at slot l % 8 of row l / 8.
   const bf16_t *sa[NA][2], *sb[NB][2];
@@ -487,17 +489,9 @@ __device__ __forceinline__ void wide_tile_mma(const GemmKArgs &p, const TileId &
     const int rh = (u * 8 + wave) * 8 + (lane >> 3);  // row of the half tile
     const int q = wide_slot(rh, lane & 7);
 #pragma unroll
-    for (int h = 0; h < NA; ++h) {
-      const int r = h * 128 + rh;
-      const int rr = row0 + (r < valid ? r : 0);  // padding rows re-read the first one, never stored
-      const long long arow = GATE_UP ? (long long)p.row_token[rr] : (long long)rr;
-      sa[h][u] = p.A + arow * p.lda + (long long)k0 * kWideBK + q * 8;
-    }
+    for (int h = 0; h < NA; ++h) sa[h][u] = row_a(h * 128 + rh) + (long long)k0 * kWideBK + q * 8;
 #pragma unroll
-    for (int g = 0; g < NB; ++g) {
-      const int wrow = GATE_UP ? (g & 1) * p.inter + (t.nt + (g >> 1)) * 128 + rh : t.nt * kWideBN + g * 128 + rh;
-      sb[g][u] = Wg + (long long)wrow * p.ldw + (long long)k0 * kWideBK + q * 8;
-    }
+    for (int g = 0; g < NB; ++g) sb[g][u] = row_b(g, rh) + (long long)k0 * kWideBK + q * 8;
   }
   const uint32_t lds0 = lds_addr(smem) + wave * 1024;
 #pragma unroll
@@ -891,11 +885,21 @@ __device__ __forceinline__ void wide_gemm(const GemmKArgs &p, int G, bf16_t *sme
     else                                                                                       \
       wide_store<GATE_UP, DBL_>(p, t, row0, valid, acc);                                       \
   } while (0)
-#define EXF_W_MAIN(DBL_, TMV_) wide_tile_mma<GATE_UP, DBL_, TMV_>(p, t, row0, valid, k0, k1, smem, acc)
+  const bf16_t *Wg = (t.g < p.n_experts) ? p.W + (long long)t.g * p.w_stride : p.Ws;
+  int valid = 0;
+  auto row_a = [&](int r) {
+    const int rr = row0 + (r < valid ? r : 0);  // padding rows re-read the first one, never stored
+    return p.A + (GATE_UP ? (long long)p.row_token[rr] : (long long)rr) * p.lda;
+  };
+  auto row_b = [&](int g, int rh) {
+    const int wrow = GATE_UP ? (g & 1) * p.inter + (t.nt + (g >> 1)) * 128 + rh : t.nt * kWideBN + g * 128 + rh;
+    return Wg + (long long)wrow * p.ldw;
+  };
+#define EXF_W_MAIN(DBL_, TMV_) wide_tile_mma<DBL_, TMV_>(row_a, row_b, k0, k1, smem, acc)
   // the 32-row blocks 64 i + 32 wm of 128 rows, `rows` of which hold rows of the group
   auto live = [&](int rows) { return max(0, min(2, (rows - 32 * (wave >> 2) + 63) >> 6)); };
   if (__builtin_amdgcn_readfirstlane(t.dbl)) {
-    const int valid = min(kWide / 2, p.offsets[t.g + 1] - row0);
+    valid = min(kWide / 2, p.offsets[t.g + 1] - row0);
     switch (live(valid)) {
       case 2: EXF_W_MAIN(true, 2); break;
       case 1: EXF_W_MAIN(true, 1); break;
@@ -903,7 +907,7 @@ __device__ __forceinline__ void wide_gemm(const GemmKArgs &p, int G, bf16_t *sme
     }
     EXF_W_STORE(true);
   } else {
-    const int valid = min(kWide, p.offsets[t.g + 1] - row0);  // more than 128
+    valid = min(kWide, p.offsets[t.g + 1] - row0);  // more than 128
     switch (2 + live(valid - 128)) {
       case 4: EXF_W_MAIN(false, 4); break;
       case 3: EXF_W_MAIN(false, 3); break;
@@ -1542,6 +1546,75 @@ hipError_t launch_plain_gemm_nt(const void *A, const void *W, int M, int N, int 
   // 2048: 14.4 -> 12.0)
   const int grid = (M + 63) / 64 * g.n_tiles * P;
   expert_gemm_tile<64, 128, false, false, true><<<grid, 256, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Matrix product with an epilogue (exfold_linear_forward) on the wide tile: 256 rows x 256
+// weight rows (gated: the gate and the up rows of 128 columns).  Tiles run in panels of
+// kLinPanel m-tiles, m-tile fastest, so that the workgroups of an XCD share both operands.
+// ---------------------------------------------------------------------------
+constexpr int kLinPanel = 8;
+
+template <bool GATED>
+__global__ __launch_bounds__(64 * kWideWaves, 1) void linear_wide(const LinearArgs a) {
+  __shared__ __attribute__((aligned(1024))) bf16_t smem[kWideSmemElems];
+  constexpr int COLS = GATED ? kWideBN / 2 : kWideBN;
+  const int mts = (a.M + kWide - 1) / kWide, nts = (a.N + COLS - 1) / COLS;
+  const int L = xcd_remap(blockIdx.x, mts * nts);
+  const int panel = L / (kLinPanel * nts), in_panel = L % (kLinPanel * nts);
+  const int pm = min(kLinPanel, mts - panel * kLinPanel);
+  const int mt = panel * kLinPanel + in_panel % pm, nt = in_panel / pm;
+  const int valid = min(kWide, a.M - mt * kWide);
+  const bf16_t *x = static_cast<const bf16_t *>(a.x), *w = static_cast<const bf16_t *>(a.w);
+  // rows past the ends re-read the last one
+  auto row_a = [&](int r) { return x + min(mt * kWide + r, a.M - 1) * a.ldx; };
+  auto row_b = [&](int g, int rh) {
+    const int wrow = GATED ? g * a.N + min(nt * COLS + rh, a.N - 1) : min(nt * COLS + g * 128 + rh, a.N - 1);
+    return w + wrow * a.ldw;
+  };
+  f32x16 acc[kWideTM][kWideTN];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  switch (2 + max(0, min(2, (valid - 128 - 32 * wm + 63) >> 6))) {
+    case 4: wide_tile_mma<false, 4>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
+    case 3: wide_tile_mma<false, 3>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
+    default: wide_tile_mma<false, 2>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
+  }
+  auto finish = [&](auto out) {
+    using O = decltype(out);
+    const bool quad = quads<O>(a);
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < kWideTM; ++i) {
+        const int ml = wide_row<false>(wm, i) + (lane & 31);
+        if (ml >= valid) continue;
+#pragma unroll
+        for (int j = 0; j < (GATED ? 1 : kWideTN); ++j)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int n = nt * COLS + wide_col<false>(wn, i, j) + 8 * g + 4 * (lane >> 5);
+            if (n >= a.N) continue;
+            float z[4], u[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              z[e] = acc[i][j][4 * g + e];
+              if constexpr (GATED) u[e] = acc[i][1][4 * g + e];
+            }
+            finish4<decltype(act)::value, GATED, O>(a, quad, mt * kWide + ml, n, z, u);
+          }
+      }
+    });
+  };
+  if (a.out_dtype == EXFOLD_F32)
+    finish(float{});
+  else
+    finish(bf16_t{});
+}
+
+hipError_t launch_linear_wide(const LinearArgs &a, const LinearPlan &p, hipStream_t s) {
+  if (a.gated) linear_wide<true><<<p.grid, 64 * kWideWaves, 0, s>>>(a);
+  else linear_wide<false><<<p.grid, 64 * kWideWaves, 0, s>>>(a);
   return hipGetLastError();
 }
 

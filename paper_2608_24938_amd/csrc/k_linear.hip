@@ -3,103 +3,9 @@
 // float32 sums, one rounding to y's type.
 #include "common.hpp"
 #include "kernels.hpp"
+#include "linear_epilogue.hpp"
 
 namespace exfold {
-
-// ---------------------------------------------------------------------------
-// Epilogue.
-// ---------------------------------------------------------------------------
-
-// FAST: the result is rounded to bf16, where the hardware's exponential and reciprocal
-// (a few float32 ulps) change nothing that the rounding keeps.
-template <bool FAST> __device__ __forceinline__ float sigmoid_times(float z, float u) {
-  if constexpr (FAST)
-    return z * __builtin_amdgcn_rcpf(1.0f + __expf(-u));
-  else
-    return z / (1.0f + expf(-u));
-}
-template <int ACT, bool FAST> __device__ __forceinline__ float activate(float z) {
-  if constexpr (ACT == EXFOLD_ACT_RELU) return z > 0.f ? z : 0.f;
-  if constexpr (ACT == EXFOLD_ACT_SILU) return sigmoid_times<FAST>(z, z);
-  if constexpr (ACT == EXFOLD_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-  // 0.5 z (1 + tanh u) = z / (1 + exp(-2 u)), u = sqrt(2 / pi) (z + 0.044715 z^3)
-  if constexpr (ACT == EXFOLD_ACT_GELU_TANH)
-    return sigmoid_times<FAST>(z, z * fmaf(0.07135481f * z, z, 1.59576912f));
-  return z;
-}
-
-// Runs f with the activation as a compile-time constant (one uniform branch a tile).
-template <typename F> __device__ __forceinline__ void with_act(int act, F f) {
-  switch (act) {
-    case EXFOLD_ACT_RELU: f(std::integral_constant<int, EXFOLD_ACT_RELU>{}); break;
-    case EXFOLD_ACT_SILU: f(std::integral_constant<int, EXFOLD_ACT_SILU>{}); break;
-    case EXFOLD_ACT_GELU: f(std::integral_constant<int, EXFOLD_ACT_GELU>{}); break;
-    case EXFOLD_ACT_GELU_TANH: f(std::integral_constant<int, EXFOLD_ACT_GELU_TANH>{}); break;
-    default: f(std::integral_constant<int, EXFOLD_ACT_NONE>{}); break;
-  }
-}
-
-// Outputs (m, n) .. (m, n + 3) from their sums z (gated: gate sums z, up sums u); columns
-// from a.N on are not touched.  quad: r and y move four values at a time.
-template <int ACT, bool GATED, typename O>
-__device__ __forceinline__ void finish4(const LinearArgs &a, bool quad, long long m, int n, const float (&z)[4],
-                                        const float (&u)[4]) {
-  constexpr bool FAST = sizeof(O) == 2;
-  O *y = static_cast<O *>(a.y) + m * a.ldy + n;
-  const O *r = a.res ? static_cast<const O *>(a.res) + m * a.ldr + n : nullptr;
-  const bool whole = quad && n + 4 <= a.N;
-  float rv[4] = {0.f, 0.f, 0.f, 0.f}, o[4];
-  if (r) {
-    if (whole) {
-      if constexpr (sizeof(O) == 2) {
-        const uint2 q = *reinterpret_cast<const uint2 *>(r);
-        rv[0] = __uint_as_float(q.x << 16);
-        rv[1] = __uint_as_float(q.x & 0xffff0000u);
-        rv[2] = __uint_as_float(q.y << 16);
-        rv[3] = __uint_as_float(q.y & 0xffff0000u);
-      } else {
-        const f32x4 q = *reinterpret_cast<const f32x4 *>(r);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) rv[e] = q[e];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (n + e < a.N) rv[e] = load_f32(r + e);
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int c = min(n + e, a.N - 1);
-    float g = z[e], v = u[e];
-    if (a.bias) {
-      g += a.bias[c];
-      if (GATED) v += a.bias[a.N + c];
-    }
-    g = activate<ACT, FAST>(g);
-    if (GATED) g *= v;
-    o[e] = g + rv[e];
-  }
-  if (whole) {
-    if constexpr (sizeof(O) == 2) {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      *reinterpret_cast<bf16x4 *>(y) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
-    } else {
-      *reinterpret_cast<f32x4 *>(y) = f32x4{o[0], o[1], o[2], o[3]};
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < a.N) y[e] = store_cvt<O>(o[e]);
-  }
-}
-
-// Whether rows of r and y can be moved four values at a time.
-template <typename O> __device__ __forceinline__ bool quads(const LinearArgs &a) {
-  const uintptr_t at = reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.res) |
-                       (uintptr_t)(a.ldy * sizeof(O)) | (uintptr_t)(a.res ? a.ldr * sizeof(O) : 0);
-  return at % (4 * sizeof(O)) == 0;
-}
 
 // ---------------------------------------------------------------------------
 // Tiles of BM rows x BN weight rows (gated: BN / 2 gate rows and the BN / 2 up rows of the
@@ -281,6 +187,127 @@ __global__ __launch_bounds__(256, 1) void linear_tile(const LinearArgs a, const 
     finish(bf16_t{});
 }
 
+// ---------------------------------------------------------------------------
+// Few rows (serving a token or four): the weights are read once and nothing is staged.  A
+// workgroup takes RW weight rows (gated: RW / 2 columns' gate and up rows) over the whole
+// reduction, its 256 threads on consecutive 16-byte pieces of each (element loads where the
+// rows allow no pieces), two sweeps of loads in flight, products in float32 on the vector
+// units; the threads' sums are added by DPP within rows of 16 lanes and then in order through
+// LDS.
+// ---------------------------------------------------------------------------
+// Elements of a 16-byte piece as float32.
+template <typename E> __device__ __forceinline__ void unpack_piece(const u32x4 &v, float (&f)[16 / sizeof(E)]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if constexpr (sizeof(E) == 2) {
+      f[2 * q] = __uint_as_float(v[q] << 16);
+      f[2 * q + 1] = __uint_as_float(v[q] & 0xffff0000u);
+    } else {
+      f[q] = __uint_as_float(v[q]);
+    }
+  }
+}
+
+// Sum over the 16 lanes of a DPP row; every lane of the row gets it.
+__device__ __forceinline__ float row_sum(float v) {
+  v += __uint_as_float(dpp_u32<0xB1>(__float_as_uint(v), 0u));
+  v += __uint_as_float(dpp_u32<0x4E>(__float_as_uint(v), 0u));
+  v += __uint_as_float(dpp_u32<0x141>(__float_as_uint(v), 0u));
+  v += __uint_as_float(dpp_u32<0x140>(__float_as_uint(v), 0u));
+  return v;
+}
+
+template <typename E, int MT, int RW, bool GATED, bool VEC>
+__global__ __launch_bounds__(256) void linear_few(const LinearArgs a) {
+  constexpr int EP = 16 / sizeof(E), U = 2, COLS = GATED ? RW / 2 : RW;
+  __shared__ float part[16][RW * MT];
+  const int tid = threadIdx.x, n0 = blockIdx.x * COLS;
+  const E *x = static_cast<const E *>(a.x), *w = static_cast<const E *>(a.w);
+  const E *xr[MT], *wr[RW];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) xr[m] = x + (long long)min(m, a.M - 1) * a.ldx;
+#pragma unroll
+  for (int r = 0; r < RW; ++r) {
+    const int n = min(n0 + (GATED ? r % COLS : r), a.N - 1);
+    wr[r] = w + (long long)(GATED && r >= COLS ? a.N + n : n) * a.ldw;
+  }
+  float acc[RW][MT];
+#pragma unroll
+  for (int r = 0; r < RW; ++r)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[r][m] = 0.f;
+  if constexpr (VEC) {
+    for (int k = tid * EP; k < a.K; k += 256 * EP * U) {
+      u32x4 wv[U][RW], xv[U][MT];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int ku = k + u * 256 * EP;
+        const bool in = ku < a.K;
+#pragma unroll
+        for (int r = 0; r < RW; ++r) wv[u][r] = in ? *reinterpret_cast<const u32x4 *>(wr[r] + ku) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xv[u][m] = in ? *reinterpret_cast<const u32x4 *>(xr[m] + ku) : u32x4{0u, 0u, 0u, 0u};
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float xf[MT][EP];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) unpack_piece<E>(xv[u][m], xf[m]);
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+          float wf[EP];
+          unpack_piece<E>(wv[u][r], wf);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int e = 0; e < EP; ++e) acc[r][m] = fmaf(wf[e], xf[m][e], acc[r][m]);
+        }
+      }
+    }
+  } else {
+    constexpr int UE = 4;
+    for (int k = tid; k < a.K; k += 256 * UE) {
+      E wv[UE][RW], xv[UE][MT];
+#pragma unroll
+      for (int u = 0; u < UE; ++u) {
+        const int ku = k + u * 256;
+        const bool in = ku < a.K;
+#pragma unroll
+        for (int r = 0; r < RW; ++r) wv[u][r] = in ? wr[r][ku] : E(0);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xv[u][m] = in ? xr[m][ku] : E(0);
+      }
+#pragma unroll
+      for (int u = 0; u < UE; ++u)
+#pragma unroll
+        for (int r = 0; r < RW; ++r)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[r][m] = fmaf(load_f32(&wv[u][r]), load_f32(&xv[u][m]), acc[r][m]);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RW; ++r)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const float v = row_sum(acc[r][m]);
+      if ((tid & 15) == 0) part[tid >> 4][m * RW + r] = v;
+    }
+  __syncthreads();
+  if (tid >= COLS * MT) return;
+  const int m = tid / COLS, c = tid % COLS, n = n0 + c;
+  if (m >= a.M || n >= a.N) return;
+  float z = 0.f, g = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    z += part[i][m * RW + c];
+    if (GATED) g += part[i][m * RW + COLS + c];
+  }
+  if (sizeof(E) == 4 || a.out_dtype == EXFOLD_F32)
+    finish1<GATED, float>(a, m, n, z, g);
+  else if constexpr (sizeof(E) == 2)
+    finish1<GATED, bf16_t>(a, m, n, z, g);
+}
+
 // Joins the split partial sums in order, four columns a thread, and finishes them.
 template <bool GATED, typename O>
 __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int ksplit) {
@@ -306,8 +333,31 @@ __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int kspli
 // ---------------------------------------------------------------------------
 // Planning and launch.
 // ---------------------------------------------------------------------------
+constexpr int kFewRows = 4;
+
 LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int cu_count) {
   LinearPlan p{};
+  p.ksplit = 1;
+  p.kc = K;
+  const long long wrows = (long long)N * (gated ? 2 : 1);
+  if (M <= kFewRows) {
+    p.kind = kLinFew;
+    p.bm = M <= 1 ? 1 : M <= 2 ? 2 : 4;
+    p.bn = wrows >= 16LL * cu_count ? 8 : 2;
+    const int cols = gated ? p.bn / 2 : p.bn;
+    p.grid = (N + cols - 1) / cols;
+    return p;
+  }
+  if (dtype == EXFOLD_BF16 && vec && K % 64 == 0 && K >= 128) {
+    // 256 x 256 tiles, one a CU, where they fill the chip
+    const long long tiles = (long long)((M + 255) / 256) * ((wrows + 255) / 256);
+    if (4 * tiles >= 3 * cu_count) {
+      p.kind = kLinWide;
+      p.bm = p.bn = 256;
+      p.grid = (int)tiles;
+      return p;
+    }
+  }
   p.kind = kLinTile;
   p.bm = 64;
   p.bn = 128;
@@ -324,15 +374,32 @@ LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int
 }
 
 template <typename E, bool GATED, bool VEC>
-static void launch_tile(const LinearArgs &a, const LinearPlan &p, hipStream_t s) {
-  linear_tile<E, 64, 128, GATED, VEC><<<p.grid, 256, 0, s>>>(a, p);
+static void launch_few(const LinearArgs &a, const LinearPlan &p, hipStream_t s) {
+  auto go = [&](auto mt) {
+    constexpr int MT = decltype(mt)::value;
+    if (p.bn == 8) linear_few<E, MT, 8, GATED, VEC><<<p.grid, 256, 0, s>>>(a);
+    else linear_few<E, MT, 2, GATED, VEC><<<p.grid, 256, 0, s>>>(a);
+  };
+  if (p.bm == 1) go(std::integral_constant<int, 1>{});
+  else if (p.bm == 2) go(std::integral_constant<int, 2>{});
+  else go(std::integral_constant<int, 4>{});
+}
+
+template <typename E, bool GATED, bool VEC>
+static void launch_typed(const LinearArgs &a, const LinearPlan &p, hipStream_t s) {
+  if (p.kind == kLinFew) launch_few<E, GATED, VEC>(a, p, s);
+  else linear_tile<E, 64, 128, GATED, VEC><<<p.grid, 256, 0, s>>>(a, p);
 }
 
 hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, bool vec, hipStream_t s) {
   if (a.M <= 0) return hipSuccess;
-  auto tile = [&](auto e, auto gated, auto v) { launch_tile<decltype(e), decltype(gated)::value, decltype(v)::value>(a, p, s); };
-  auto by_vec = [&](auto e, auto gated) { vec ? tile(e, gated, std::true_type{}) : tile(e, gated, std::false_type{}); };
-  auto by_gate = [&](auto e) { a.gated ? by_vec(e, std::true_type{}) : by_vec(e, std::false_type{}); };
+  if (p.kind == kLinWide) return launch_linear_wide(a, p, s);
+  auto typed = [&](auto e, auto gated) {
+    using E = decltype(e);
+    constexpr bool G = decltype(gated)::value;
+    vec ? launch_typed<E, G, true>(a, p, s) : launch_typed<E, G, false>(a, p, s);
+  };
+  auto by_gate = [&](auto e) { a.gated ? typed(e, std::true_type{}) : typed(e, std::false_type{}); };
   if (a.dtype == EXFOLD_BF16) by_gate(bf16_t{}); else by_gate(float{});
   if (p.ksplit > 1) {
     const long long n = (long long)a.M * ((a.N + 3) / 4);

@@ -63,8 +63,9 @@ struct LinearArgs {
   bool gated;
   float *part;  // [ksplit][M][linear_part_ld] float32 partial sums, when split
 };
-// Kernel families of the product.
-enum { kLinTile = 0 };
+// kLinFew: vector products of a few rows; kLinTile: MFMA tiles of four waves; kLinWide:
+// the 256 x 256 tiles of the expert GEMMs (bf16).
+enum { kLinFew = 0, kLinTile = 1, kLinWide = 2 };
 struct LinearPlan {
   int kind;
   int bm, bn;  // tile rows, and weight rows of a tile
@@ -76,6 +77,7 @@ struct LinearPlan {
 LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int cu_count);
 __host__ __device__ inline long long linear_part_ld(int N, bool gated) { return ((long long)N * (gated ? 2 : 1) + 3) / 4 * 4; }
 hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, bool vec, hipStream_t s);
+hipError_t launch_linear_wide(const LinearArgs &a, const LinearPlan &p, hipStream_t s);  // k_gemm.hip
 
 // ---- permutation (k_permute.hip) ----
 constexpr int kPermSlotsPerBlock = 1024;

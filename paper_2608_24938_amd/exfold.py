@@ -407,35 +407,46 @@ def calibrate_diagonal(layer: Layer, x_cal, lam: float = 1e-3, mode: str = "coro
 
 
 _DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)   # the handle without the Stream object's 2.5 us
 
 
 def _matrix(t, name, dtype=None, shape=None, device=None):
     """Row stride of a 2-D GPU tensor whose rows are contiguous (gaps between rows allowed)."""
-    if t.dim() != 2 or not t.is_cuda or t.dtype not in _DTYPE or (t.shape[1] > 1 and t.stride(1) != 1) \
-            or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != shape) \
+    sh = t.shape
+    if len(sh) != 2 or not t.is_cuda or t.dtype not in _DTYPE or (sh[1] > 1 and t.stride(1) != 1) \
+            or (dtype is not None and t.dtype != dtype) or (shape is not None and sh != shape) \
             or (device is not None and t.device != device):
         raise ValueError(f"{name}: expected a 2-D {dtype or 'float32 or bfloat16'} tensor"
-                         f"{'' if shape is None else f' {shape}'} with contiguous rows on "
-                         f"{'the GPU' if device is None else device}, got {t.dtype} {tuple(t.shape)} with strides "
+                         f"{'' if shape is None else f' {tuple(shape)}'} with contiguous rows on "
+                         f"{'the GPU' if device is None else device}, got {t.dtype} {tuple(sh)} with strides "
                          f"{t.stride()} on {t.device}")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0) if sh[0] > 1 else sh[1]
 
 
 def _vector(t, n, name, device):
-    if t is not None and (t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous() or t.device != device):
+    """Address of a float32 vector of n entries, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name}: expected contiguous float32 ({n},) on {device}, got {t.dtype} {tuple(t.shape)} "
                          f"on {t.device}")
+    return t.data_ptr()
 
 
 def _call_on(device, stream, where, fn, *args):
-    """fn(*args, stream) on the tensors' device: the given stream, or that device's current one."""
+    """fn(*args, stream) with the tensors' device current, on the given stream or that device's current one."""
     if stream is not None and stream.device != device:
         raise ValueError(f"{where}: the stream is on {stream.device}, the tensors on {device}")
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(stream)), where)
-        return
-    with torch.cuda.device(device):
-        _check(fn(*args, _stream(stream)), where)
+    index = device.index
+    handle = _raw_stream(index) if stream is None else stream.cuda_stream
+    if index == torch.cuda.current_device():
+        status = fn(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, handle)
+    if status != OK:
+        raise ExfoldError(status, where)
 
 
 def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, keep_groups=1, group_top2=False,
@@ -450,43 +461,32 @@ def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, ke
     ld = _matrix(logits, "logits")
     T, N = logits.shape
     dev = logits.device
-    _vector(select_bias, N, "select_bias", dev)
+    bias = _vector(select_bias, N, "select_bias", dev)
     if score not in SCORE:
         raise ValueError(f"score: expected one of {sorted(SCORE)}, got {score!r}")
     if topk_ids is None:
-        topk_ids = torch.empty((T, top_k), dtype=torch.int32, device=dev)
+        topk_ids = logits.new_empty((T, top_k), dtype=torch.int32)
     else:
         _need(topk_ids, torch.int32, (T, top_k), "topk_ids")
     if topk_w is None:
-        topk_w = torch.empty((T, top_k), dtype=torch.float32, device=dev)
+        topk_w = logits.new_empty((T, top_k), dtype=torch.float32)
     else:
         _need(topk_w, torch.float32, (T, top_k), "topk_w")
     if topk_ids.device != dev or topk_w.device != dev:
         raise ValueError(f"topk_ids, topk_w: expected on {dev}")
-    r = _Routing(SCORE[score], 1 if group_top2 else 0, groups, keep_groups, 1 if renorm else 0, scale,
-                 None if select_bias is None else select_bias.data_ptr())
+    r = _Routing(SCORE[score], 1 if group_top2 else 0, groups, keep_groups, 1 if renorm else 0, scale, bias)
     _call_on(dev, stream, "exfold_route_experts", lib().exfold_route_experts, ctypes.byref(r), logits.data_ptr(),
              _DTYPE[logits.dtype], ld, T, N, top_k, topk_ids.data_ptr(), topk_w.data_ptr())
     return topk_ids, topk_w
 
 
-def _linear_struct(w, ldw, n_out, bias, act, gated, out_dtype):
-    if act not in ACT:
-        raise ValueError(f"act: expected one of {sorted(ACT)}, got {act!r}")
-    if out_dtype not in _DTYPE:
-        raise ValueError(f"out_dtype: expected float32 or bfloat16, got {out_dtype}")
-    return _Linear(w.shape[1], n_out, ldw, w.data_ptr(), None if bias is None else bias.data_ptr(), _DTYPE[w.dtype],
-                   _DTYPE[out_dtype], ACT[act], 1 if gated else 0)
-
-
 def linear_workspace_size(w, rows, gated=False) -> int:
-    """Bytes of workspace of linear() for `rows` rows of x and this weight."""
+    """Bytes of workspace that linear() of `rows` rows of x and this weight needs (0: none)."""
+    ldw = _matrix(w, "w")
     n_out = w.shape[0] // 2 if gated else w.shape[0]
-    ls = _linear_struct(w, _matrix(w, "w"), n_out, None, "none", gated, w.dtype)
-    n = lib().exfold_linear_workspace_size(ctypes.byref(ls), rows)
-    if n == 0:
-        raise ValueError("invalid shape for exfold_linear_forward")
-    return n
+    code = _DTYPE[w.dtype]
+    ls = _Linear(w.shape[1], n_out, ldw, w.data_ptr(), None, code, code, 0, 1 if gated else 0)
+    return lib().exfold_linear_workspace_size(ctypes.byref(ls), rows)
 
 
 def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=None, y=None, workspace=None, stream=None):
@@ -495,28 +495,40 @@ def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=No
     x [M, n_in] and w [n_out, n_in] (gated: [2 n_out, n_in], gate rows first) of one type, float32 or
     bfloat16, rows contiguous; bias [n_out] (gated [2 n_out]) float32; residual and y [M, n_out] of
     out_dtype (x's type unless given; float32 is always allowed).  y may be the residual (y += ...).
-    act: "none", "relu", "silu", "gelu" or "gelu_tanh".  workspace: linear_workspace_size bytes, made here
-    unless given."""
+    act: "none", "relu", "silu", "gelu" or "gelu_tanh".  workspace: a tensor of at least
+    linear_workspace_size bytes; made here, where one is needed, unless given."""
     ldx = _matrix(x, "x")
-    dev = x.device
+    dev, dtype = x.device, x.dtype
     M, K = x.shape
-    rows = w.shape[0] if w.dim() == 2 else 0
-    if gated and rows % 2:
-        raise ValueError(f"w: a gated product has as many gate as up rows, got {rows} rows")
-    ldw = _matrix(w, "w", x.dtype, (rows, K), dev)
-    n_out = rows // 2 if gated else rows
-    _vector(bias, rows, "bias", dev)
+    ldw = _matrix(w, "w", dtype, None, dev)
+    rows, kw = w.shape
+    n_out = rows
+    if gated:
+        if rows % 2:
+            raise ValueError(f"w: a gated product has as many gate as up rows, got {rows} rows")
+        n_out = rows // 2
+    if kw != K:
+        raise ValueError(f"w: expected rows of {K} elements, those of x, got {kw}")
+    b = _vector(bias, rows, "bias", dev)
     if out_dtype is None:
-        out_dtype = x.dtype if y is None else y.dtype
-    ldr = 0 if residual is None else _matrix(residual, "residual", out_dtype, (M, n_out), dev)
+        out_dtype = dtype if y is None else y.dtype
+    if out_dtype not in _DTYPE:
+        raise ValueError(f"out_dtype: expected float32 or bfloat16, got {out_dtype}")
+    if act not in ACT:
+        raise ValueError(f"act: expected one of {sorted(ACT)}, got {act!r}")
+    res, ldr = None, 0
+    if residual is not None:
+        ldr, res = _matrix(residual, "residual", out_dtype, (M, n_out), dev), residual.data_ptr()
     if y is None:
-        y = torch.empty((M, n_out), dtype=out_dtype, device=dev)
-    ldy = _matrix(y, "y", out_dtype, (M, n_out), dev)
-    ls = _linear_struct(w, ldw, n_out, bias, act, gated, out_dtype)
-    p = ctypes.byref(ls)
+        y, ldy = x.new_empty((M, n_out), dtype=out_dtype), n_out
+    else:
+        ldy = _matrix(y, "y", out_dtype, (M, n_out), dev)
+    p = ctypes.byref(_Linear(K, n_out, ldw, w.data_ptr(), b, _DTYPE[dtype], _DTYPE[out_dtype], ACT[act], 1 if gated else 0))
     if workspace is None:
-        workspace = _workspace(lib().exfold_linear_workspace_size(p, M), dev, stream)
-    _call_on(dev, stream, "exfold_linear_forward", lib().exfold_linear_forward, p, x.data_ptr(), ldx, M,
-             None if residual is None else residual.data_ptr(), ldr, y.data_ptr(), ldy, workspace.data_ptr(),
-             workspace.numel() * workspace.element_size())
+        need = lib().exfold_linear_workspace_size(p, M)
+        if need:
+            workspace = _workspace(need, dev, stream)
+    ws, nbytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _call_on(dev, stream, "exfold_linear_forward", lib().exfold_linear_forward, p, x.data_ptr(), ldx, M, res, ldr,
+             y.data_ptr(), ldy, ws, nbytes)
     return y

@@ -52,7 +52,7 @@ XP, WP, BP, RP, YP, WS = F, 64 * F, 128 * F, 192 * F, 256 * F, 320 * F
 
 
 def linear(M=4, x=XP, ldx=None, res=None, ldr=0, y=YP, ldy=None, ws=WS, ws_bytes=None, lin=True, **kw):
-    a = dict(n_in=64, n_out=32, ldw=None, w=WP, bias=None, dtype=X.BF16, out_dtype=None, act=0, gated=0)
+    a = dict(n_in=4096, n_out=32, ldw=None, w=WP, bias=None, dtype=X.BF16, out_dtype=None, act=0, gated=0)
     a.update(kw)
     a["ldw"] = a["n_in"] if a["ldw"] is None else a["ldw"]
     a["out_dtype"] = a["dtype"] if a["out_dtype"] is None else a["out_dtype"]
@@ -72,10 +72,10 @@ def linear(M=4, x=XP, ldx=None, res=None, ldr=0, y=YP, ldy=None, ws=WS, ws_bytes
     (dict(out_dtype=5), X.ERR_DTYPE, False),
     (dict(act=5), X.ERR_ARG, False), (dict(act=-1), X.ERR_ARG, False), (dict(gated=2), X.ERR_ARG, False),
     (dict(n_in=0), X.ERR_SHAPE, False), (dict(n_out=0), X.ERR_SHAPE, False), (dict(n_in=(1 << 17) + 1), X.ERR_SHAPE, False),
-    (dict(n_out=(1 << 17) + 1), X.ERR_SHAPE, False), (dict(ldw=63), X.ERR_SHAPE, False),
+    (dict(n_out=(1 << 17) + 1), X.ERR_SHAPE, False), (dict(ldw=4095), X.ERR_SHAPE, False),
     (dict(ldw=(1 << 31) + 1), X.ERR_SHAPE, False), (dict(M=-1), X.ERR_SHAPE, False),
     (dict(M=(1 << 22) + 1), X.ERR_SHAPE, False), (dict(M=1 << 22, n_out=1 << 13), X.ERR_SHAPE, False),
-    (dict(ldx=63), X.ERR_SHAPE, True), (dict(ldy=31), X.ERR_SHAPE, True), (dict(res=RP, ldr=31), X.ERR_SHAPE, True),
+    (dict(ldx=4095), X.ERR_SHAPE, True), (dict(ldy=31), X.ERR_SHAPE, True), (dict(res=RP, ldr=31), X.ERR_SHAPE, True),
     (dict(ldx=(1 << 31) + 1), X.ERR_SHAPE, True), (dict(ldy=(1 << 31) + 1), X.ERR_SHAPE, True),
     (dict(w=WP + 1), X.ERR_ALIGN, False), (dict(bias=BP + 2), X.ERR_ALIGN, False), (dict(x=XP + 1), X.ERR_ALIGN, True),
     (dict(y=YP + 1), X.ERR_ALIGN, True), (dict(out_dtype=X.F32, y=YP + 2), X.ERR_ALIGN, True),
@@ -84,12 +84,19 @@ def linear(M=4, x=XP, ldx=None, res=None, ldr=0, y=YP, ldy=None, ws=WS, ws_bytes
     (dict(y=XP), X.ERR_ARG, True), (dict(y=WP + 2), X.ERR_ARG, True), (dict(y=BP + 4, bias=BP), X.ERR_ARG, True),
     (dict(y=YP, res=YP + 2, ldr=32), X.ERR_ARG, True), (dict(y=YP, res=YP, ldr=64), X.ERR_ARG, True),
     (dict(y=WS + 16), X.ERR_ARG, True), (dict(x=WS - 16), X.ERR_ARG, True),
-    (dict(y=XP + 2 * 40, ldx=96, ldy=96), X.ERR_ARG, True),               # columns 40 .. 71 of rows of 64
+    (dict(y=XP + 2 * 4090, ldx=4200, ldy=4200), X.ERR_ARG, True),         # from x's column 4090 on
 ])
 def test_linear_refusals(kw, code, sized):
     st, size = linear(**kw)
     assert st == code
     assert (size > 0) == sized
+
+
+def test_linear_needs_a_workspace_only_for_partial_sums():
+    assert linear(x=None)[1] > 0                                          # 4096 long, one tile of outputs
+    st, size = linear(n_in=64, x=None, ws=None)
+    assert (st, size) == (X.ERR_NULL, 0)
+    assert linear(n_in=64, n_out=1 << 15, x=None, ws=None)[1] == 0
 
 
 def test_linear_no_rows_is_a_no_op():
