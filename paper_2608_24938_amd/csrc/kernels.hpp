@@ -49,6 +49,7 @@ struct RouteExpertsArgs {
   const float *bias;  // [N] selection bias, or nullptr
   int32_t *ids;       // [T, K]
   float *w;           // [T, K]
+  bool vec;           // set by the launch: rows are read in 16-byte pieces
 };
 hipError_t launch_route_experts(const RouteExpertsArgs &a, hipStream_t s);
 
