@@ -796,16 +796,12 @@ exfold_status check_linear(const exfold_linear *L, int64_t M) {
   return EXFOLD_OK;
 }
 
-size_t linear_need(const exfold_linear *L, int64_t M) {
-  size_t need = 0;
-  for (int vec = 0; vec < 2; ++vec) {  // what the pointers and strides of the call allow
-    const LinearPlan p = plan_linear(L->dtype, L->gated != 0, vec != 0, (int)M, (int)L->n_out, (int)L->n_in, cu_count());
-    if (p.ksplit > 1) {
-      const size_t bytes = sizeof(float) * (size_t)p.ksplit * M * linear_part_ld((int)L->n_out, L->gated != 0);
-      if (align_up(bytes) > need) need = align_up(bytes);
-    }
-  }
-  return need;
+LinearPlan linear_plan(const exfold_linear *L, int64_t M, bool vec) {
+  return plan_linear(L->dtype, L->gated != 0, vec, (int)M, (int)L->n_out, (int)L->n_in, cu_count());
+}
+size_t linear_need(const exfold_linear *L, int64_t M, const LinearPlan &p) {
+  if (p.ksplit <= 1) return 0;
+  return align_up(sizeof(float) * (size_t)p.ksplit * M * linear_part_cols((int)L->n_out) * (L->gated ? 2 : 1));
 }
 
 }  // namespace
@@ -854,7 +850,11 @@ exfold_status exfold_route_experts(const exfold_routing *r, const void *logits, 
 }
 
 size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M) {
-  return check_linear(linear, M) == EXFOLD_OK ? linear_need(linear, M) : 0;
+  if (check_linear(linear, M) != EXFOLD_OK || M == 0) return 0;
+  // whatever the pointers and strides of the call allow
+  const size_t pieces = linear_need(linear, M, linear_plan(linear, M, true));
+  const size_t any = linear_need(linear, M, linear_plan(linear, M, false));
+  return pieces > any ? pieces : any;
 }
 
 exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64_t ldx, int64_t M,
@@ -868,7 +868,9 @@ exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64
   if (!x || !y) return EXFOLD_ERR_NULL;
   const int64_t esz = (int64_t)element(L->dtype), osz = (int64_t)element(L->out_dtype);
   if (unaligned_to(x, esz) || unaligned_to(y, osz) || unaligned_to(residual, osz)) return EXFOLD_ERR_ALIGN;
-  const size_t need = linear_need(L, M);
+  const bool vec = !misaligned(x) && !misaligned(L->w) && ldx * esz % 16 == 0 && L->ldw * esz % 16 == 0 && L->n_in * esz % 16 == 0;
+  const LinearPlan p = linear_plan(L, M, vec);
+  const size_t need = linear_need(L, M, p);
   if (need > 0) {
     st = check_ws(ws, ws_bytes, need);
     if (st != EXFOLD_OK) return st;
@@ -898,8 +900,6 @@ exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64
   a.act = L->act;
   a.gated = L->gated != 0;
   a.part = static_cast<float *>(ws);
-  const bool vec = !misaligned(x) && !misaligned(L->w) && ldx * esz % 16 == 0 && L->ldw * esz % 16 == 0 && L->n_in * esz % 16 == 0;
-  const LinearPlan p = plan_linear(a.dtype, a.gated, vec, a.M, a.N, a.K, cu_count());
   return launch_linear(a, p, vec, static_cast<hipStream_t>(stream)) == hipSuccess ? EXFOLD_OK : EXFOLD_ERR_DEVICE;
 }
 

@@ -1581,28 +1581,25 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void linear_wide(const LinearAr
     case 3: wide_tile_mma<false, 3>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
     default: wide_tile_mma<false, 2>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
   }
+  // runs of four columns of a row: 4 j + g
+  constexpr int NQ = GATED ? 4 : 8;
+  auto col = [&](int q) { return nt * COLS + wide_col<false>(wn, 0, q >> 2) + 8 * (q & 3) + 4 * (lane >> 5); };
+  f32x4 bz[NQ], bu[NQ];
+  bias_quads<GATED>(a, col, bz, bu);
   auto finish = [&](auto out) {
-    using O = decltype(out);
-    const bool quad = quads<O>(a);
     with_act(a.act, [&](auto act) {
 #pragma unroll
       for (int i = 0; i < kWideTM; ++i) {
         const int ml = wide_row<false>(wm, i) + (lane & 31);
         if (ml >= valid) continue;
+        finish_row<decltype(act)::value, GATED, decltype(out)>(
+            a, mt * kWide + ml, bz, bu, col, [&](int q, f32x4 &z, f32x4 &u) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < (GATED ? 1 : kWideTN); ++j)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int n = nt * COLS + wide_col<false>(wn, i, j) + 8 * g + 4 * (lane >> 5);
-            if (n >= a.N) continue;
-            float z[4], u[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              z[e] = acc[i][j][4 * g + e];
-              if constexpr (GATED) u[e] = acc[i][1][4 * g + e];
-            }
-            finish4<decltype(act)::value, GATED, O>(a, quad, mt * kWide + ml, n, z, u);
-          }
+              for (int e = 0; e < 4; ++e) {
+                z[e] = acc[i][GATED ? 0 : q >> 2][4 * (q & 3) + e];
+                if constexpr (GATED) u[e] = acc[i][1][4 * q + e];
+              }
+            });
       }
     });
   };

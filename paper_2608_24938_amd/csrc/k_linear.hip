@@ -18,82 +18,127 @@ namespace exfold {
 // consecutive ones a wave.  Rows past the ends re-read the last one and are not stored;
 // columns past K are zero.
 // ---------------------------------------------------------------------------
-template <typename E> __device__ __forceinline__ void mma32(const u32x4 &a, const u32x4 &b, f32x16 &c) {
-  if constexpr (sizeof(E) == 2) {
+template <typename E> constexpr int mma_steps() { return sizeof(E) == 2 ? 1 : 4; }
+template <typename E> __device__ __forceinline__ void mma32(const u32x4 &a, const u32x4 &b, int e, f32x16 &c) {
+  if constexpr (sizeof(E) == 2)
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
-  }
+  else
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
 }
 
 // LDS slot (16-byte units) of piece q of tile row r (8 pieces a row).
 __device__ __forceinline__ int piece_at(int r, int q) { return r * 8 + (q ^ ((r ^ (r >> 1)) & 7)); }
 
-template <typename E, int BM, int BN, bool GATED, bool VEC>
-__global__ __launch_bounds__(256, 1) void linear_tile(const LinearArgs a, const LinearPlan p) {
-  constexpr int KS = 128 / sizeof(E), EP = 16 / sizeof(E);
-  constexpr int TM = BM / 64, TN = BN / 64;
-  constexpr int PA = BM * 8 / 256, PB = BN * 8 / 256;                 // pieces a thread
-  constexpr int SA = VEC ? 1 : BM * KS / 256, SB = VEC ? 1 : BN * KS / 256;  // elements a thread
+// Sums of a wave's TM x TN tiles to the outputs, or to the partial sums of split ks.  Register r
+// of tile (i, j): row row0 + arow(i) + lane % 32, tile column brow(j) + 8 (r / 4) + 4 (lane / 32)
+// + r % 4 (the weights are the MFMA's first operand): runs of four columns.
+template <typename E, int TM, int TN, int COLS, bool GATED, typename RowA, typename RowB>
+__device__ __forceinline__ void tile_epilogue(const LinearArgs &a, const LinearPlan &p, int row0, int nt, int ks, int lane,
+                                              const f32x16 (&acc)[TM][TN], const RowA &arow, const RowB &brow) {
+  auto quad = [&](int i, int q) __attribute__((always_inline)) {  // run q of row block i
+    const f32x16 &c = acc[i][q >> 2];
+    return f32x4{c[4 * (q & 3)], c[4 * (q & 3) + 1], c[4 * (q & 3) + 2], c[4 * (q & 3) + 3]};
+  };
+  auto at = [&](int q) { return brow(q >> 2) + 8 * (q & 3) + 4 * (lane >> 5); };  // its tile column
+  if (p.ksplit > 1) {
+    const int np = linear_part_cols(a.N);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m = row0 + arow(i) + (lane & 31);
+      if (m >= a.M) continue;
+      float *row = a.part + ((long long)ks * a.M + m) * np * (GATED ? 2 : 1);
+#pragma unroll
+      for (int q = 0; q < 4 * TN; ++q) {
+        const int c = at(q), n = nt * COLS + (GATED ? c & (COLS - 1) : c);
+        if (n < a.N) *reinterpret_cast<f32x4 *>(row + (GATED && c >= COLS ? np : 0) + n) = quad(i, q);
+      }
+    }
+    return;
+  }
+  constexpr int NQ = GATED ? 2 * TN : 4 * TN;
+  auto col = [&](int q) { return nt * COLS + at(q); };
+  f32x4 bz[NQ], bu[NQ];
+  bias_quads<GATED>(a, col, bz, bu);
+  auto finish = [&](auto out) {
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int m = row0 + arow(i) + (lane & 31);
+        if (m >= a.M) continue;
+        finish_row<decltype(act)::value, GATED, decltype(out)>(
+            a, m, bz, bu, col, [&](int q, f32x4 &z, f32x4 &u) __attribute__((always_inline)) {
+              z = quad(i, q);
+              if constexpr (GATED) u = quad(i, q + NQ);
+            });
+      }
+    });
+  };
+  if (sizeof(E) == 4 || a.out_dtype == EXFOLD_F32)
+    finish(float{});
+  else if constexpr (sizeof(E) == 2)
+    finish(bf16_t{});
+}
+
+// A 16-byte piece of a row at any element alignment, `left` elements of which exist (the rest 0).
+template <typename E> __device__ __forceinline__ u32x4 load_piece(const E *p, int left) {
+  constexpr int EP = 16 / sizeof(E);
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (left >= EP) {
+    __builtin_memcpy(&v, p, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < EP - 1; ++e)
+      if (e < left) {
+        if constexpr (sizeof(E) == 2) v[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+        else v[e] = __float_as_uint(p[e]);
+      }
+  }
+  return v;
+}
+
+template <typename E, int BM, int BN, bool GATED>
+__global__ __launch_bounds__(256, 2) void linear_tile(const LinearArgs a, const LinearPlan p) {
+  constexpr int EP = 16 / sizeof(E), KS = 8 * EP;
+  constexpr int TM = BM / 64, TN = BN / 64, COLS = GATED ? BN / 2 : BN;
+  constexpr int PA = BM * 8 / 256, PB = BN * 8 / 256;  // pieces a thread
   static_assert(!GATED || TN % 2 == 0, "a wave holds the gate and the up columns");
   __shared__ __attribute__((aligned(16))) u32x4 smem[2][(BM + BN) * 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
-  const int mts = (a.M + BM - 1) / BM, cols = GATED ? BN / 2 : BN, nts = (a.N + cols - 1) / cols;
+  const int mts = (a.M + BM - 1) / BM, nts = (a.N + COLS - 1) / COLS;
   const int L = xcd_remap(blockIdx.x, mts * nts * p.ksplit);
   const int mt = L % mts, nt = L / mts % nts, ks = L / mts / nts;
-  const int k0 = ks * p.kc, k1 = min(a.K, k0 + p.kc);
-  const E *x = static_cast<const E *>(a.x), *w = static_cast<const E *>(a.w);
-  // weight row of tile row r
-  auto wrow = [&](int r) {
-    if (!GATED) return min(nt * BN + r, a.N - 1);
-    const int c = min(nt * (BN / 2) + (r & (BN / 2 - 1)), a.N - 1);
-    return r < BN / 2 ? c : a.N + c;
-  };
-  auto xrow = [&](int r) { return min(mt * BM + r, a.M - 1); };
-
-  const E *sa[VEC ? PA : 1], *sb[VEC ? PB : 1];
-  if constexpr (VEC) {
+  const int k0 = ks * p.kc, k1 = min(a.K, k0 + p.kc), kq = (tid & 7) * EP;
+  const E *sa[PA], *sb[PB];
 #pragma unroll
-    for (int i = 0; i < PA; ++i) sa[i] = x + xrow(i * 32 + (tid >> 3)) * a.ldx + (tid & 7) * EP;
+  for (int i = 0; i < PA; ++i)
+    sa[i] = static_cast<const E *>(a.x) + min(mt * BM + i * 32 + (tid >> 3), a.M - 1) * a.ldx + kq;
 #pragma unroll
-    for (int i = 0; i < PB; ++i) sb[i] = w + wrow(i * 32 + (tid >> 3)) * a.ldw + (tid & 7) * EP;
+  for (int i = 0; i < PB; ++i) {
+    const int r = i * 32 + (tid >> 3), c = min(nt * COLS + (GATED ? r & (COLS - 1) : r), a.N - 1);
+    sb[i] = static_cast<const E *>(a.w) + (GATED && r >= COLS ? a.N + c : c) * a.ldw + kq;
   }
-  u32x4 ra[VEC ? PA : 1], rb[VEC ? PB : 1];
-  E ea[SA], eb[SB];
-  auto load = [&](int k) __attribute__((always_inline)) {
-    if constexpr (VEC) {
-      const bool in = k + (tid & 7) * EP < k1;
+  // two register sets: the loads of a stage fly during the MFMAs of the two before it
+  u32x4 ra0[PA], rb0[PB], ra1[PA], rb1[PB];
+  auto load = [&](int k, u32x4 (&ra)[PA], u32x4 (&rb)[PB]) __attribute__((always_inline)) {
+    const int left = k1 - k - kq;
+    if (k + KS <= k1) {
 #pragma unroll
-      for (int i = 0; i < PA; ++i) ra[i] = in ? *reinterpret_cast<const u32x4 *>(sa[i] + k) : u32x4{0u, 0u, 0u, 0u};
+      for (int i = 0; i < PA; ++i) __builtin_memcpy(&ra[i], sa[i] + k, 16);
 #pragma unroll
-      for (int i = 0; i < PB; ++i) rb[i] = in ? *reinterpret_cast<const u32x4 *>(sb[i] + k) : u32x4{0u, 0u, 0u, 0u};
+      for (int i = 0; i < PB; ++i) __builtin_memcpy(&rb[i], sb[i] + k, 16);
     } else {
-      const int c = tid % KS, r0 = tid / KS;
-      const bool in = k + c < k1;
 #pragma unroll
-      for (int i = 0; i < SA; ++i) ea[i] = in ? x[xrow(r0 + i * (256 / KS)) * a.ldx + k + c] : E(0);
+      for (int i = 0; i < PA; ++i) ra[i] = load_piece(sa[i] + k, left);
 #pragma unroll
-      for (int i = 0; i < SB; ++i) eb[i] = in ? w[wrow(r0 + i * (256 / KS)) * a.ldw + k + c] : E(0);
+      for (int i = 0; i < PB; ++i) rb[i] = load_piece(sb[i] + k, left);
     }
   };
-  auto stage = [&](int buf) __attribute__((always_inline)) {
+  auto stage = [&](int buf, const u32x4 (&ra)[PA], const u32x4 (&rb)[PB]) __attribute__((always_inline)) {
     u32x4 *As = smem[buf], *Bs = As + BM * 8;
-    if constexpr (VEC) {
 #pragma unroll
-      for (int i = 0; i < PA; ++i) As[piece_at(i * 32 + (tid >> 3), tid & 7)] = ra[i];
+    for (int i = 0; i < PA; ++i) As[piece_at(i * 32 + (tid >> 3), tid & 7)] = ra[i];
 #pragma unroll
-      for (int i = 0; i < PB; ++i) Bs[piece_at(i * 32 + (tid >> 3), tid & 7)] = rb[i];
-    } else {
-      const int c = tid % KS, r0 = tid / KS;
-#pragma unroll
-      for (int i = 0; i < SA; ++i)
-        reinterpret_cast<E *>(&As[piece_at(r0 + i * (256 / KS), c / EP)])[c % EP] = ea[i];
-#pragma unroll
-      for (int i = 0; i < SB; ++i)
-        reinterpret_cast<E *>(&Bs[piece_at(r0 + i * (256 / KS), c / EP)])[c % EP] = eb[i];
-    }
+    for (int i = 0; i < PB; ++i) Bs[piece_at(i * 32 + (tid >> 3), tid & 7)] = rb[i];
   };
   f32x16 acc[TM][TN];
 #pragma unroll
@@ -103,88 +148,243 @@ __global__ __launch_bounds__(256, 1) void linear_tile(const LinearArgs a, const 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   // tile row of a wave's column block j: blocks wn, wn + 2, ... (gated: gate and up blocks in step)
+  auto arow = [&](int i) { return (i * 2 + wm) * 32; };
   auto brow = [&](int j) { return (j * 2 + wn) * 32; };
-
-  int buf = 0;
-  load(k0);
-  stage(0);
-  __syncthreads();
-  for (int k = k0; k < k1; k += KS) {
-    const bool more = k + KS < k1;
-    if (more) load(k + KS);
+  auto multiply = [&](int buf) __attribute__((always_inline)) {
     const u32x4 *As = smem[buf], *Bs = As + BM * 8;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       u32x4 fa[TM], fb[TN];
 #pragma unroll
-      for (int i = 0; i < TM; ++i) fa[i] = As[piece_at((i * 2 + wm) * 32 + (lane & 31), 2 * s + (lane >> 5))];
+      for (int i = 0; i < TM; ++i) fa[i] = As[piece_at(arow(i) + (lane & 31), 2 * s + (lane >> 5))];
 #pragma unroll
       for (int j = 0; j < TN; ++j) fb[j] = Bs[piece_at(brow(j) + (lane & 31), 2 * s + (lane >> 5))];
 #pragma unroll
+      for (int e = 0; e < mma_steps<E>(); ++e)
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) mma32<E>(fb[j], fa[i], e, acc[i][j]);
+    }
+  };
+  load(k0, ra0, rb0);
+  load(k0 + KS, ra1, rb1);
+  stage(0, ra0, rb0);
+  __syncthreads();
+  for (int k = k0; k < k1; k += 2 * KS) {
+    load(k + 2 * KS, ra0, rb0);
+    multiply(0);
+    stage(1, ra1, rb1);
+    __syncthreads();
+    if (k + KS >= k1) break;
+    load(k + 3 * KS, ra1, rb1);
+    multiply(1);
+    stage(0, ra0, rb0);
+    __syncthreads();
+  }
+  tile_epilogue<E, TM, TN, COLS, GATED>(a, p, mt * BM, nt, ks, lane, acc, arow, brow);
+}
+
+// ---------------------------------------------------------------------------
+// Ring tiles (rows in 16-byte pieces, more than four of them): BM rows x BN weight rows as
+// above, but the stages go from global memory straight into an LDS ring of S buffers, S - 1
+// stages ahead, with one barrier a stage: a wave waits until its own loads of the stage have
+// landed and its LDS reads of the last one have ended, meets the others, refills the buffer
+// they all have left, and multiplies.  Stages past the end of the range, and pieces past K,
+// read zeros from a constant, so that every wave has the same number of loads in flight at
+// every wait.
+// KW: the four waves take one 16-byte step of a stage each on the whole tile instead of a
+// quarter of the tile (few rows: the tile is small and the weights stream), and their sums are
+// added in wave order through LDS.
+// ONCE: one tile of rows, so no other workgroup reads these weights: non-temporal loads (16
+// rows on 28672 x 4096 weights 48.1 -> 42.6 us; 8 on 4096 x 4096, which fit the last-level
+// cache, 11.8 -> 11.5).
+// ---------------------------------------------------------------------------
+__device__ const u32x4 kZeroPiece[8] = {};
+
+// One 16-byte piece a lane from global g into the 1 KiB LDS block at byte address lds
+// (wave-uniform): lane l lands at lds + 16 l.  M0 holds the block address; nothing else in
+// these kernels uses M0 (no indirect register moves).
+template <bool ONCE> __device__ __forceinline__ void ring_load(const char *g, uint32_t lds) {
+  if constexpr (ONCE)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(g), "s"(lds) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(lds) : "memory", "m0");
+}
+
+// Sum of the four waves' values at red (wave-major, BM rows of PITCH floats each), in wave order.
+template <int BM, int PITCH> __device__ __forceinline__ f32x4 kw_sum(const float *red) {
+  f32x4 v = *reinterpret_cast<const f32x4 *>(red);
+#pragma unroll
+  for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4 *>(red + w * BM * PITCH);
+  return v;
+}
+
+template <typename E, int BM, int BN, int S, bool KW, bool GATED, bool ONCE>
+__global__ __launch_bounds__(256, BM == 128 ? 1 : 2) void linear_ring(const LinearArgs a, const LinearPlan p) {
+  constexpr int EP = 16 / sizeof(E), KS = 8 * EP, ROWS = BM + BN, NB = ROWS / 32;
+  constexpr int TM = KW ? BM / 32 : BM / 64, TN = KW ? BN / 32 : BN / 64;
+  constexpr int COLS = GATED ? BN / 2 : BN;
+  static_assert(!GATED || TN % 2 == 0, "a wave holds the gate and the up columns");
+  constexpr int PITCH = BN + 4;  // floats of a row of the waves' sums
+  constexpr int RING = S * ROWS * 8, RED = KW ? 4 * BM * PITCH / 4 : 0;
+  __shared__ __attribute__((aligned(1024))) u32x4 smem[RING > RED ? RING : RED];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = KW ? 0 : wave >> 1, wn = KW ? 0 : wave & 1;
+  const int mts = (a.M + BM - 1) / BM, nts = (a.N + COLS - 1) / COLS;
+  const int L = xcd_remap(blockIdx.x, mts * nts * p.ksplit);
+  const int mt = L % mts, nt = L / mts % nts, ks = L / mts / nts;
+  const int k0 = ks * p.kc, k1 = min(a.K, k0 + p.kc), stages = (k1 - k0 + KS - 1) / KS;
+
+  // 1 KiB block i of this wave: rows 8 (4 i + wave) .. + 7 of the stage, x rows first
+  const char *src[NB];
+  int kq[NB];  // this lane's piece of the row, in elements
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int r = 8 * (4 * i + wave) + (lane >> 3), q = (lane & 7) ^ ((r ^ (r >> 1)) & 7);
+    const E *row;
+    if (i < BM / 32) {
+      row = static_cast<const E *>(a.x) + min(mt * BM + r, a.M - 1) * a.ldx;
+    } else {
+      const int b = r - BM, c = min(nt * COLS + (GATED ? b & (COLS - 1) : b), a.N - 1);
+      row = static_cast<const E *>(a.w) + (GATED && b >= COLS ? a.N + c : c) * a.ldw;
+    }
+    kq[i] = k0 + q * EP;
+    src[i] = reinterpret_cast<const char *>(row + kq[i]);
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)smem + wave * 1024;
+  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
+    const uint32_t to = lds0 + slot * (ROWS * 128);
+    if (st < stages - 1) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        if (i < BM / 32) ring_load<false>(src[i] + (long long)st * 128, to + i * 4096);
+        else ring_load<ONCE>(src[i] + (long long)st * 128, to + i * 4096);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        ring_load<false>(kq[i] + st * KS < k1 ? src[i] + (long long)st * 128 : reinterpret_cast<const char *>(kZeroPiece), to + i * 4096);
+    }
+  };
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  auto arow = [&](int i) { return KW ? i * 32 : (i * 2 + wm) * 32; };
+  auto brow = [&](int j) { return KW ? j * 32 : (j * 2 + wn) * 32; };
+
+  constexpr int STEPS = KW ? 1 : 4;
+  u32x4 fa[TM], fb[TN], na[TM], nb[TN];  // fragments of a step and of the next
+  // byte offsets in a buffer of this lane's piece of step s in the wave's first row blocks; the
+  // others are whole blocks further (the swizzle repeats every 16 rows)
+  uint32_t at_a[STEPS], at_b[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int q = 2 * (KW ? wave : s) + (lane >> 5);
+    at_a[s] = piece_at(arow(0) + (lane & 31), q) * 16;
+    at_b[s] = (BM * 8 + piece_at(brow(0) + (lane & 31), q)) * 16;
+  }
+  constexpr int STEP_ROWS = KW ? 32 : 64;
+  auto read = [&](int slot, int s, u32x4 (&ra)[TM], u32x4 (&rb)[TN]) __attribute__((always_inline)) {
+    const char *base = reinterpret_cast<const char *>(smem) + slot * (ROWS * 128);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) rb[j] = *reinterpret_cast<const u32x4 *>(base + at_b[s] + j * STEP_ROWS * 128);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) ra[i] = *reinterpret_cast<const u32x4 *>(base + at_a[s] + i * STEP_ROWS * 128);
+    __builtin_amdgcn_sched_barrier(0);  // read now: the products of the step before cover the latency
+  };
+  auto multiply = [&](const u32x4 (&ra)[TM], const u32x4 (&rb)[TN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < mma_steps<E>(); ++e)
+#pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) mma32<E>(fb[j], fa[i], acc[i][j]);
-    }
-    if (more) stage(buf ^ 1);
-    __syncthreads();
-    buf ^= 1;
-  }
-
-  // Register r of tile (i, j): row (i 2 + wm) 32 + lane % 32, column brow(j) + 8 (r / 4) +
-  // 4 (lane / 32) + r % 4 (the weights are the MFMA's first operand): runs of four columns.
-  const int m0 = mt * BM + wm * 32 + (lane & 31);
-  if (p.ksplit > 1) {
-    const long long ld = linear_part_ld(a.N, GATED);
-    const int nw = GATED ? 2 * a.N : a.N;
+        for (int j = 0; j < TN; ++j) mma32<E>(rb[j], ra[i], e, acc[i][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int m = m0 + i * 64;
-      if (m >= a.M) continue;
-      float *row = a.part + ((long long)ks * a.M + m) * ld;
+  for (int st = 0; st < S; ++st) issue(st, st);
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((S - 1) * NB) : "memory");
+  read(0, 0, fa, fb);
+  int slot = 0;
+  for (int st = 0; st < stages; ++st) {
+#pragma unroll
+    for (int s = 0; s < STEPS - 1; s += 2) {
+      read(slot, s + 1, na, nb);
+      multiply(fa, fb);
+      if (s + 2 < STEPS) {
+        read(slot, s + 2, fa, fb);
+        multiply(na, nb);
+      }
+    }
+    // the next stage has landed and this one is read: its buffer is filled again
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((S - 2) * NB) : "memory");
+    issue(st + S, slot);
+    slot = slot == S - 1 ? 0 : slot + 1;
+    if constexpr (STEPS > 1) {
+      read(slot, 0, fa, fb);
+      multiply(na, nb);
+    } else {
+      read(slot, 0, na, nb);
+      multiply(fa, fb);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) fa[i] = na[i];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb[j] = nb[j];
+    }
+  }
+  // no load into the ring is left, and every wave has read it
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+
+  if constexpr (!KW) {
+    tile_epilogue<E, TM, TN, COLS, GATED>(a, p, mt * BM, nt, ks, lane, acc, arow, brow);
+  } else {
+    float *red = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int c = brow(j) + 8 * g + 4 * (lane >> 5);
-          const int in_half = GATED ? nt * (BN / 2) + (c & (BN / 2 - 1)) : nt * BN + c;
-          const int base = GATED && c >= BN / 2 ? a.N : 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (in_half + e < a.N) row[base + in_half + e] = acc[i][j][4 * g + e];
-        }
-    }
-    (void)nw;
-    return;
-  }
-  auto finish = [&](auto out) {
-    using O = decltype(out);
-    const bool quad = quads<O>(a);
-    with_act(a.act, [&](auto act) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const int m = m0 + i * 64;
-        if (m >= a.M) continue;
-#pragma unroll
-        for (int j = 0; j < (GATED ? TN / 2 : TN); ++j)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int n = nt * cols + brow(j) + 8 * g + 4 * (lane >> 5);
-            if (n >= a.N) continue;
-            float z[4], u[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              z[e] = acc[i][j][4 * g + e];
-              if constexpr (GATED) u[e] = acc[i][j + TN / 2][4 * g + e];
-            }
-            finish4<decltype(act)::value, GATED, O>(a, quad, m, n, z, u);
-          }
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4 *>(red + (wave * BM + i * 32 + (lane & 31)) * PITCH + j * 32 + 8 * g + 4 * (lane >> 5)) =
+              f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    __syncthreads();
+    if (p.ksplit > 1) {
+      const int np = linear_part_cols(a.N);
+      float *part = a.part + (long long)ks * a.M * np * (GATED ? 2 : 1);
+      for (int i = tid; i < BM * BN / 4; i += 256) {
+        const int ml = i / (BN / 4), c = i % (BN / 4) * 4, m = mt * BM + ml, n = nt * COLS + (GATED ? c & (COLS - 1) : c);
+        if (m < a.M && n < a.N)
+          *reinterpret_cast<f32x4 *>(part + (long long)m * np * (GATED ? 2 : 1) + (GATED && c >= COLS ? np : 0) + n) =
+              kw_sum<BM, PITCH>(red + ml * PITCH + c);
       }
-    });
-  };
-  if (sizeof(E) == 4 || a.out_dtype == EXFOLD_F32)
-    finish(float{});
-  else if constexpr (sizeof(E) == 2)
-    finish(bf16_t{});
+      return;
+    }
+    // run i of this thread: row tid / (COLS / 4) + i of as many rows as 256 threads cover
+    constexpr int QN = COLS / 4, RN = 256 / QN;
+    const int n = nt * COLS + tid % QN * 4;
+    auto col = [&](int) { return n; };
+    f32x4 bz[1], bu[1];
+    bias_quads<GATED>(a, col, bz, bu);
+    auto finish = [&](auto out) {
+      with_act(a.act, [&](auto act) {
+        for (int ml = tid / QN; ml < BM && mt * BM + ml < a.M; ml += RN)
+          finish_row<decltype(act)::value, GATED, decltype(out)>(
+              a, mt * BM + ml, bz, bu, col, [&](int, f32x4 &z, f32x4 &u) __attribute__((always_inline)) {
+                z = kw_sum<BM, PITCH>(red + ml * PITCH + tid % QN * 4);
+                if constexpr (GATED) u = kw_sum<BM, PITCH>(red + ml * PITCH + COLS + tid % QN * 4);
+              });
+      });
+    };
+    if (sizeof(E) == 4 || a.out_dtype == EXFOLD_F32)
+      finish(float{});
+    else if constexpr (sizeof(E) == 2)
+      finish(bf16_t{});
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -236,53 +436,36 @@ __global__ __launch_bounds__(256) void linear_few(const LinearArgs a) {
   for (int r = 0; r < RW; ++r)
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[r][m] = 0.f;
-  if constexpr (VEC) {
-    for (int k = tid * EP; k < a.K; k += 256 * EP * U) {
-      u32x4 wv[U][RW], xv[U][MT];
+  auto piece = [&](const E *row, int k) {
+    if constexpr (VEC)
+      return k < a.K ? *reinterpret_cast<const u32x4 *>(row + k) : u32x4{0u, 0u, 0u, 0u};
+    else
+      return load_piece(row + k, a.K - k);
+  };
+  for (int k = tid * EP; k < a.K; k += 256 * EP * U) {
+    u32x4 wv[U][RW], xv[U][MT];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int ku = k + u * 256 * EP;
-        const bool in = ku < a.K;
+    for (int u = 0; u < U; ++u) {
+      const int ku = k + u * 256 * EP;
 #pragma unroll
-        for (int r = 0; r < RW; ++r) wv[u][r] = in ? *reinterpret_cast<const u32x4 *>(wr[r] + ku) : u32x4{0u, 0u, 0u, 0u};
+      for (int r = 0; r < RW; ++r) wv[u][r] = piece(wr[r], ku);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) xv[u][m] = in ? *reinterpret_cast<const u32x4 *>(xr[m] + ku) : u32x4{0u, 0u, 0u, 0u};
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float xf[MT][EP];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) unpack_piece<E>(xv[u][m], xf[m]);
-#pragma unroll
-        for (int r = 0; r < RW; ++r) {
-          float wf[EP];
-          unpack_piece<E>(wv[u][r], wf);
-#pragma unroll
-          for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int e = 0; e < EP; ++e) acc[r][m] = fmaf(wf[e], xf[m][e], acc[r][m]);
-        }
-      }
+      for (int m = 0; m < MT; ++m) xv[u][m] = piece(xr[m], ku);
     }
-  } else {
-    constexpr int UE = 4;
-    for (int k = tid; k < a.K; k += 256 * UE) {
-      E wv[UE][RW], xv[UE][MT];
 #pragma unroll
-      for (int u = 0; u < UE; ++u) {
-        const int ku = k + u * 256;
-        const bool in = ku < a.K;
+    for (int u = 0; u < U; ++u) {
+      float xf[MT][EP];
 #pragma unroll
-        for (int r = 0; r < RW; ++r) wv[u][r] = in ? wr[r][ku] : E(0);
+      for (int m = 0; m < MT; ++m) unpack_piece<E>(xv[u][m], xf[m]);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) xv[u][m] = in ? xr[m][ku] : E(0);
+      for (int r = 0; r < RW; ++r) {
+        float wf[EP];
+        unpack_piece<E>(wv[u][r], wf);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int e = 0; e < EP; ++e) acc[r][m] = fmaf(wf[e], xf[m][e], acc[r][m]);
       }
-#pragma unroll
-      for (int u = 0; u < UE; ++u)
-#pragma unroll
-        for (int r = 0; r < RW; ++r)
-#pragma unroll
-          for (int m = 0; m < MT; ++m) acc[r][m] = fmaf(load_f32(&wv[u][r]), load_f32(&xv[u][m]), acc[r][m]);
     }
   }
 #pragma unroll
@@ -311,23 +494,28 @@ __global__ __launch_bounds__(256) void linear_few(const LinearArgs a) {
 // Joins the split partial sums in order, four columns a thread, and finishes them.
 template <bool GATED, typename O>
 __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int ksplit) {
-  const long long ld = linear_part_ld(a.N, GATED), split = (long long)a.M * ld;
-  const int quads_n = (a.N + 3) / 4;
+  const int np = linear_part_cols(a.N), quads_n = np / 4;
+  const long long ld = (long long)np * (GATED ? 2 : 1), split = a.M * ld;
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   if (i >= (long long)a.M * quads_n) return;
   const long long m = i / quads_n;
   const int n = (int)(i % quads_n) * 4;
-  const float *row = a.part + m * ld;
-  float z[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < ksplit; ++s)
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < a.N) {
-        z[e] += row[s * split + n + e];
-        if (GATED) u[e] += row[s * split + a.N + n + e];
-      }
-  const bool quad = quads<O>(a);
-  with_act(a.act, [&](auto act) { finish4<decltype(act)::value, GATED, O>(a, quad, m, n, z, u); });
+  const float *row = a.part + m * ld + n;
+  f32x4 zs = {0.f, 0.f, 0.f, 0.f}, us = zs;
+#pragma unroll 4
+  for (int s = 0; s < ksplit; ++s) {
+    zs += *reinterpret_cast<const f32x4 *>(row + s * split);
+    if (GATED) us += *reinterpret_cast<const f32x4 *>(row + s * split + np);
+  }
+  auto col = [&](int) { return n; };
+  f32x4 bz[1], bu[1];
+  bias_quads<GATED>(a, col, bz, bu);
+  with_act(a.act, [&](auto act) {
+    finish_row<decltype(act)::value, GATED, O>(a, m, bz, bu, col, [&](int, f32x4 &z, f32x4 &u) {
+      z = zs;
+      u = us;
+    });
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -335,10 +523,29 @@ __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int kspli
 // ---------------------------------------------------------------------------
 constexpr int kFewRows = 4;
 
+// Tiles and what a stage of one takes a CU that holds one workgroup of them or several in
+// turn (measured, microseconds).  bf16: the bytes of the stage at about 65 GB/s a CU, wide
+// tiles by their MFMAs; float32: the MFMAs.  The register-staged tiles wait for their loads,
+// and two workgroups a CU overlap.
+struct TileCost {
+  int kind, bm, bn;
+  float bf16, f32;
+};
+constexpr TileCost kTiles[] = {{kLinRing, 32, 64, 0.19f, 0.375f}, {kLinRing, 64, 64, 0.24f, 0.66f},
+                               {kLinRing, 64, 128, 0.36f, 1.16f}, {kLinRing, 128, 128, 0.52f, 2.33f},
+                               {kLinWide, 256, 256, 1.6f, 0.f},   {kLinTile, 64, 128, 1.1f, 1.6f}};
+
+// The tile and split of the least estimated time: rounds of tiles over the CUs, or the
+// weights' and rows' bytes from memory (about 4.8 TB/s) where those take longer, and for a
+// split its partial sums, written and read, and the launch that joins them.  The estimate
+// picks among kernels that all are right; it is within 20% of what they measured (600 x 2048
+// x 768 float32: 32 us on 32 x 64 tiles, 34 on 64 x 128, 57 on 128 x 128; 64 x 4096 x 4096
+// bf16: 13.4 us split in four, 15.3 not).
 LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int cu_count) {
   LinearPlan p{};
   p.ksplit = 1;
   p.kc = K;
+  const bool bf16 = dtype == EXFOLD_BF16;
   const long long wrows = (long long)N * (gated ? 2 : 1);
   if (M <= kFewRows) {
     p.kind = kLinFew;
@@ -348,28 +555,40 @@ LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int
     p.grid = (N + cols - 1) / cols;
     return p;
   }
-  if (dtype == EXFOLD_BF16 && vec && K % 64 == 0 && K >= 128) {
-    // 256 x 256 tiles, one a CU, where they fill the chip
-    const long long tiles = (long long)((M + 255) / 256) * ((wrows + 255) / 256);
-    if (4 * tiles >= 3 * cu_count) {
-      p.kind = kLinWide;
-      p.bm = p.bn = 256;
-      p.grid = (int)tiles;
-      return p;
+  const int stage = bf16 ? 64 : 32, stages = (K + stage - 1) / stage;
+  const double memory = ((double)wrows * K + (double)M * K) * (bf16 ? 2 : 4) / 4.8e6;  // us
+  double best = 0.0;
+  for (const TileCost &t : kTiles) {
+    if ((t.kind == kLinTile) == vec) continue;
+    if (t.kind == kLinWide && (!bf16 || K % 64 != 0 || K < 128)) continue;
+    const int cols = gated ? t.bn / 2 : t.bn;
+    const long long tiles = (long long)((M + t.bm - 1) / t.bm) * ((N + cols - 1) / cols);
+    for (int fill = 0; fill <= 2; ++fill) {  // not split, or one or two workgroups a CU
+      long long split = 1;
+      if (fill > 0) {
+        split = fill * (long long)cu_count / tiles;
+        if (split > stages / 6) split = stages / 6;
+        if (split > 32) split = 32;
+        if (split < 2 || t.kind == kLinWide) continue;
+      }
+      const int per = (int)((stages + split - 1) / split), ksplit = (stages + per - 1) / per;
+      const long long wgs = tiles * ksplit, round = t.kind == kLinTile ? 2 * cu_count : cu_count;
+      double us = (double)((wgs + round - 1) / round) * per * (bf16 ? t.bf16 : t.f32);
+      // few streams are slower, and tiles of rows drift apart, so their weights come again
+      const int again = (M + t.bm - 1) / t.bm - 1;
+      const double slow = memory * ((2 * wgs < 3 * cu_count ? 1.15 : 1.0) + 0.2 * (again < 3 ? again : 3));
+      if (us < slow && memory > 10.0) us = slow + 0.05 * us;
+      if (ksplit > 1) us += 2.5 + ksplit * (double)M * wrows * 8 / 4e6;
+      if (best > 0.0 && us >= best) continue;
+      best = us;
+      p.kind = t.kind;
+      p.bm = t.bm;
+      p.bn = t.bn;
+      p.ksplit = ksplit;
+      p.kc = ksplit > 1 ? per * stage : K;
+      p.grid = (int)(tiles * ksplit);
     }
   }
-  p.kind = kLinTile;
-  p.bm = 64;
-  p.bn = 128;
-  const int cols = gated ? p.bn / 2 : p.bn, stage = dtype == EXFOLD_BF16 ? 64 : 32;
-  const long long tiles = (long long)((M + p.bm - 1) / p.bm) * ((N + cols - 1) / cols);
-  const int stages = (K + stage - 1) / stage;
-  int split = 1;
-  while (tiles * split < cu_count && split < 16 && stages / (2 * split) >= 4) split *= 2;
-  const int per = (stages + split - 1) / split;
-  p.kc = per * stage;
-  p.ksplit = (stages + per - 1) / per;
-  p.grid = (int)(tiles * p.ksplit);
   return p;
 }
 
@@ -387,8 +606,19 @@ static void launch_few(const LinearArgs &a, const LinearPlan &p, hipStream_t s) 
 
 template <typename E, bool GATED, bool VEC>
 static void launch_typed(const LinearArgs &a, const LinearPlan &p, hipStream_t s) {
-  if (p.kind == kLinFew) launch_few<E, GATED, VEC>(a, p, s);
-  else linear_tile<E, 64, 128, GATED, VEC><<<p.grid, 256, 0, s>>>(a, p);
+  if (p.kind == kLinFew) {
+    launch_few<E, GATED, VEC>(a, p, s);
+  } else if constexpr (VEC) {
+    const bool once = a.M <= p.bm;
+    if (p.bm == 32 && once) linear_ring<E, 32, 64, 6, true, GATED, true><<<p.grid, 256, 0, s>>>(a, p);
+    else if (p.bm == 32) linear_ring<E, 32, 64, 6, true, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+    else if (p.bn == 64 && once) linear_ring<E, 64, 64, 4, true, GATED, true><<<p.grid, 256, 0, s>>>(a, p);
+    else if (p.bn == 64) linear_ring<E, 64, 64, 4, true, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+    else if (p.bm == 64) linear_ring<E, 64, 128, 3, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+    else linear_ring<E, 128, 128, 4, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+  } else {
+    linear_tile<E, 64, 128, GATED><<<p.grid, 256, 0, s>>>(a, p);
+  }
 }
 
 hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, bool vec, hipStream_t s) {
@@ -402,7 +632,7 @@ hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, bool vec, hip
   auto by_gate = [&](auto e) { a.gated ? typed(e, std::true_type{}) : typed(e, std::false_type{}); };
   if (a.dtype == EXFOLD_BF16) by_gate(bf16_t{}); else by_gate(float{});
   if (p.ksplit > 1) {
-    const long long n = (long long)a.M * ((a.N + 3) / 4);
+    const long long n = (long long)a.M * (linear_part_cols(a.N) / 4);
     const int grid = (int)((n + 255) / 256);
     auto join = [&](auto gated, auto o) { linear_join<decltype(gated)::value, decltype(o)><<<grid, 256, 0, s>>>(a, p.ksplit); };
     if (a.out_dtype == EXFOLD_BF16)

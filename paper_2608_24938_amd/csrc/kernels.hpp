@@ -62,11 +62,12 @@ struct LinearArgs {
   long long ldx, ldw, ldr, ldy;
   int M, N, K, dtype, out_dtype, act;
   bool gated;
-  float *part;  // [ksplit][M][linear_part_ld] float32 partial sums, when split
+  float *part;  // [ksplit][M][linear_part_cols (gated: twice)] float32 partial sums, when split
 };
-// kLinFew: vector products of a few rows; kLinTile: MFMA tiles of four waves; kLinWide:
-// the 256 x 256 tiles of the expert GEMMs (bf16).
-enum { kLinFew = 0, kLinTile = 1, kLinWide = 2 };
+// kLinFew: vector products of a few rows; kLinTile: MFMA tiles of four waves staged
+// through registers; kLinRing: the same through an LDS ring; kLinWide: the 256 x 256 tiles
+// of the expert GEMMs (bf16).
+enum { kLinFew = 0, kLinTile = 1, kLinRing = 2, kLinWide = 3 };
 struct LinearPlan {
   int kind;
   int bm, bn;  // tile rows, and weight rows of a tile
@@ -76,7 +77,8 @@ struct LinearPlan {
 };
 // vec: rows of x and w start on 16 bytes and K is a whole number of 16-byte pieces.
 LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int cu_count);
-__host__ __device__ inline long long linear_part_ld(int N, bool gated) { return ((long long)N * (gated ? 2 : 1) + 3) / 4 * 4; }
+// Columns of a row of partial sums (gated: the up columns follow, as many).
+__host__ __device__ inline int linear_part_cols(int N) { return (N + 3) / 4 * 4; }
 hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, bool vec, hipStream_t s);
 hipError_t launch_linear_wide(const LinearArgs &a, const LinearPlan &p, hipStream_t s);  // k_gemm.hip
 
