@@ -872,6 +872,7 @@ exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64
   const LinearPlan p = linear_plan(L, M, vec);
   const size_t need = linear_need(L, M, p);
   if (need > 0) {
+    if (!ws && ws_bytes == 0) return EXFOLD_ERR_WORKSPACE;
     st = check_ws(ws, ws_bytes, need);
     if (st != EXFOLD_OK) return st;
   }

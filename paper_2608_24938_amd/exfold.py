@@ -434,19 +434,25 @@ def _vector(t, n, name, device):
     return t.data_ptr()
 
 
-def _call_on(device, stream, where, fn, *args):
-    """fn(*args, stream) with the tensors' device current, on the given stream or that device's current one."""
-    if stream is not None and stream.device != device:
-        raise ValueError(f"{where}: the stream is on {stream.device}, the tensors on {device}")
+def _output(t, dtype, shape, name, device):
+    _need(t, dtype, shape, name)
+    if t.device != device:
+        raise ValueError(f"{name}: expected on {device}, got {t.device}")
+
+
+def _call_on(device, stream, fn, *args):
+    """Status of fn(*args, stream) with the tensors' device current, on the given stream or that device's current one."""
     index = device.index
-    handle = _raw_stream(index) if stream is None else stream.cuda_stream
-    if index == torch.cuda.current_device():
-        status = fn(*args, handle)
+    if stream is None:
+        handle = _raw_stream(index)
+    elif stream.device == device:
+        handle = stream.cuda_stream
     else:
-        with torch.cuda.device(index):
-            status = fn(*args, handle)
-    if status != OK:
-        raise ExfoldError(status, where)
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+    if index == torch.cuda.current_device():
+        return fn(*args, handle)
+    with torch.cuda.device(index):
+        return fn(*args, handle)
 
 
 def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, keep_groups=1, group_top2=False,
@@ -465,18 +471,18 @@ def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, ke
     if score not in SCORE:
         raise ValueError(f"score: expected one of {sorted(SCORE)}, got {score!r}")
     if topk_ids is None:
-        topk_ids = logits.new_empty((T, top_k), dtype=torch.int32)
+        topk_ids = torch.empty(T, top_k, dtype=torch.int32, device=dev)
     else:
-        _need(topk_ids, torch.int32, (T, top_k), "topk_ids")
+        _output(topk_ids, torch.int32, (T, top_k), "topk_ids", dev)
     if topk_w is None:
-        topk_w = logits.new_empty((T, top_k), dtype=torch.float32)
+        topk_w = torch.empty(T, top_k, dtype=torch.float32, device=dev)
     else:
-        _need(topk_w, torch.float32, (T, top_k), "topk_w")
-    if topk_ids.device != dev or topk_w.device != dev:
-        raise ValueError(f"topk_ids, topk_w: expected on {dev}")
+        _output(topk_w, torch.float32, (T, top_k), "topk_w", dev)
     r = _Routing(SCORE[score], 1 if group_top2 else 0, groups, keep_groups, 1 if renorm else 0, scale, bias)
-    _call_on(dev, stream, "exfold_route_experts", lib().exfold_route_experts, ctypes.byref(r), logits.data_ptr(),
-             _DTYPE[logits.dtype], ld, T, N, top_k, topk_ids.data_ptr(), topk_w.data_ptr())
+    status = _call_on(dev, stream, lib().exfold_route_experts, ctypes.byref(r), logits.data_ptr(), _DTYPE[logits.dtype],
+                      ld, T, N, top_k, topk_ids.data_ptr(), topk_w.data_ptr())
+    if status != OK:
+        raise ExfoldError(status, "exfold_route_experts")
     return topk_ids, topk_w
 
 
@@ -520,15 +526,19 @@ def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=No
     if residual is not None:
         ldr, res = _matrix(residual, "residual", out_dtype, (M, n_out), dev), residual.data_ptr()
     if y is None:
-        y, ldy = x.new_empty((M, n_out), dtype=out_dtype), n_out
+        y, ldy = torch.empty(M, n_out, dtype=out_dtype, device=dev), n_out
     else:
         ldy = _matrix(y, "y", out_dtype, (M, n_out), dev)
     p = ctypes.byref(_Linear(K, n_out, ldw, w.data_ptr(), b, _DTYPE[dtype], _DTYPE[out_dtype], ACT[act], 1 if gated else 0))
-    if workspace is None:
-        need = lib().exfold_linear_workspace_size(p, M)
-        if need:
-            workspace = _workspace(need, dev, stream)
-    ws, nbytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _call_on(dev, stream, "exfold_linear_forward", lib().exfold_linear_forward, p, x.data_ptr(), ldx, M, res, ldr,
-             y.data_ptr(), ldy, ws, nbytes)
+    L = lib()
+    args = (p, x.data_ptr(), ldx, M, res, ldr, y.data_ptr(), ldy)
+    if workspace is None:  # most small products need none: ask for its size only when the call does
+        status = _call_on(dev, stream, L.exfold_linear_forward, *args, None, 0)
+        if status == ERR_WORKSPACE:
+            workspace = _workspace(L.exfold_linear_workspace_size(p, M), dev, stream)
+    if workspace is not None:
+        status = _call_on(dev, stream, L.exfold_linear_forward, *args, workspace.data_ptr(),
+                          workspace.numel() * workspace.element_size())
+    if status != OK:
+        raise ExfoldError(status, "exfold_linear_forward")
     return y
