@@ -221,7 +221,7 @@ template <int BM, int PITCH> __device__ __forceinline__ f32x4 kw_sum(const float
 }
 
 template <typename E, int BM, int BN, int S, bool KW, bool GATED, bool ONCE>
-__global__ __launch_bounds__(256, BM == 128 ? 1 : 2) void linear_ring(const LinearArgs a, const LinearPlan p) {
+__global__ __launch_bounds__(256, BM == 128 && S > 2 ? 1 : 2) void linear_ring(const LinearArgs a, const LinearPlan p) {
   constexpr int EP = 16 / sizeof(E), KS = 8 * EP, ROWS = BM + BN, NB = ROWS / 32;
   constexpr int TM = KW ? BM / 32 : BM / 64, TN = KW ? BN / 32 : BN / 64;
   constexpr int COLS = GATED ? BN / 2 : BN;
@@ -587,6 +587,7 @@ LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int
       p.ksplit = ksplit;
       p.kc = ksplit > 1 ? per * stage : K;
       p.grid = (int)(tiles * ksplit);
+      p.shared_cu = p.grid > cu_count;
     }
   }
   return p;
@@ -609,12 +610,18 @@ static void launch_typed(const LinearArgs &a, const LinearPlan &p, hipStream_t s
   if (p.kind == kLinFew) {
     launch_few<E, GATED, VEC>(a, p, s);
   } else if constexpr (VEC) {
+    // Buffers: as many stages as two workgroups a CU leave room for where the loads are waited
+    // for, few where several workgroups a CU cover each other: float32 on 32 x 64 tiles (600 x
+    // 2048 x 768: three 29.0 us, six 32.2), and 128 x 128 tiles that are more than the CUs
+    // (2048 x 4096 x 4096: two 76.2 us, four 87.6; 128 x 28672 x 4096, 224 tiles: 74.6, 63.6).
+    constexpr int S32 = sizeof(E) == 4 ? 3 : 6;
     const bool once = a.M <= p.bm;
-    if (p.bm == 32 && once) linear_ring<E, 32, 64, 6, true, GATED, true><<<p.grid, 256, 0, s>>>(a, p);
-    else if (p.bm == 32) linear_ring<E, 32, 64, 6, true, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+    if (p.bm == 32 && once) linear_ring<E, 32, 64, S32, true, GATED, true><<<p.grid, 256, 0, s>>>(a, p);
+    else if (p.bm == 32) linear_ring<E, 32, 64, S32, true, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.bn == 64 && once) linear_ring<E, 64, 64, 4, true, GATED, true><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.bn == 64) linear_ring<E, 64, 64, 4, true, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.bm == 64) linear_ring<E, 64, 128, 3, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+    else if (p.shared_cu) linear_ring<E, 128, 128, 2, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else linear_ring<E, 128, 128, 4, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
   } else {
     linear_tile<E, 64, 128, GATED><<<p.grid, 256, 0, s>>>(a, p);

@@ -74,6 +74,7 @@ struct LinearPlan {
   int ksplit;  // splits of the reduction, joined by a second kernel
   int kc;      // columns of a split (the last may hold fewer)
   int grid;
+  bool shared_cu;  // more workgroups than CUs
 };
 // vec: rows of x and w start on 16 bytes and K is a whole number of 16-byte pieces.
 LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int cu_count);
