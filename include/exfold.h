@@ -460,8 +460,9 @@ typedef struct exfold_linear {
 
 /* Bytes of workspace exfold_linear_forward needs for M rows: 0 where it needs none (ws may
  * then be NULL), and on invalid input.  A call without one (NULL, 0 bytes) that needs it
- * returns EXFOLD_ERR_WORKSPACE.  It holds partial sums during the call, so calls that
- * overlap in time (other streams, graphs replayed together) need workspaces of their own. */
+ * returns EXFOLD_ERR_WORKSPACE.  It holds partial sums and copies of unaligned rows during
+ * the call, so calls that overlap in time (other streams, graphs replayed together) need
+ * workspaces of their own. */
 size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M);
 
 /*

@@ -796,12 +796,28 @@ exfold_status check_linear(const exfold_linear *L, int64_t M) {
   return EXFOLD_OK;
 }
 
-LinearPlan linear_plan(const exfold_linear *L, int64_t M, bool vec) {
-  return plan_linear(L->dtype, L->gated != 0, vec, (int)M, (int)L->n_out, (int)L->n_in, cu_count());
+// Whether rows ld elements apart start on 16 bytes.
+bool rows_aligned(const void *p, int64_t ld, int32_t dtype) {
+  return !misaligned(p) && ld * (int64_t)element(dtype) % 16 == 0;
 }
-size_t linear_need(const exfold_linear *L, int64_t M, const LinearPlan &p) {
-  if (p.ksplit <= 1) return 0;
-  return align_up(sizeof(float) * (size_t)p.ksplit * M * linear_part_cols((int)L->n_out) * (L->gated ? 2 : 1));
+LinearPlan linear_plan(const exfold_linear *L, int64_t M, bool vec_x) {
+  return plan_linear(L->dtype, L->gated != 0, vec_x, rows_aligned(L->w, L->ldw, L->dtype), (int)M, (int)L->n_out,
+                     (int)L->n_in, cu_count());
+}
+// Workspace of a call: copies of rows that are not aligned, then partial sums.
+struct LinearSpace {
+  size_t o_x = 0, o_w = 0, o_part = 0, total = 0;
+};
+LinearSpace linear_space(const exfold_linear *L, int64_t M, const LinearPlan &p) {
+  LinearSpace sp;
+  Carver c;
+  const size_t esz = element(L->dtype), rows_w = (size_t)L->n_out * (L->gated ? 2 : 1);
+  if (p.copy_x) sp.o_x = c.take(esz * M * p.K);
+  if (p.copy_w) sp.o_w = c.take(esz * rows_w * p.K);
+  if (p.ksplit > 1)
+    sp.o_part = c.take(sizeof(float) * (size_t)p.ksplit * M * linear_part_cols((int)L->n_out) * (L->gated ? 2 : 1));
+  sp.total = c.off;
+  return sp;
 }
 
 }  // namespace
@@ -851,10 +867,10 @@ exfold_status exfold_route_experts(const exfold_routing *r, const void *logits, 
 
 size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M) {
   if (check_linear(linear, M) != EXFOLD_OK || M == 0) return 0;
-  // whatever the pointers and strides of the call allow
-  const size_t pieces = linear_need(linear, M, linear_plan(linear, M, true));
-  const size_t any = linear_need(linear, M, linear_plan(linear, M, false));
-  return pieces > any ? pieces : any;
+  // whichever rows of x the call brings
+  const size_t aligned = linear_space(linear, M, linear_plan(linear, M, true)).total;
+  const size_t any = linear_space(linear, M, linear_plan(linear, M, false)).total;
+  return aligned > any ? aligned : any;
 }
 
 exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64_t ldx, int64_t M,
@@ -868,9 +884,9 @@ exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64
   if (!x || !y) return EXFOLD_ERR_NULL;
   const int64_t esz = (int64_t)element(L->dtype), osz = (int64_t)element(L->out_dtype);
   if (unaligned_to(x, esz) || unaligned_to(y, osz) || unaligned_to(residual, osz)) return EXFOLD_ERR_ALIGN;
-  const bool vec = !misaligned(x) && !misaligned(L->w) && ldx * esz % 16 == 0 && L->ldw * esz % 16 == 0 && L->n_in * esz % 16 == 0;
-  const LinearPlan p = linear_plan(L, M, vec);
-  const size_t need = linear_need(L, M, p);
+  const LinearPlan p = linear_plan(L, M, rows_aligned(x, ldx, L->dtype));
+  const LinearSpace sp = linear_space(L, M, p);
+  const size_t need = sp.total;
   if (need > 0) {
     if (!ws && ws_bytes == 0) return EXFOLD_ERR_WORKSPACE;
     st = check_ws(ws, ws_bytes, need);
@@ -900,8 +916,10 @@ exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64
   a.out_dtype = L->out_dtype;
   a.act = L->act;
   a.gated = L->gated != 0;
-  a.part = static_cast<float *>(ws);
-  return launch_linear(a, p, vec, static_cast<hipStream_t>(stream)) == hipSuccess ? EXFOLD_OK : EXFOLD_ERR_DEVICE;
+  a.copied_x = at<char>(ws, sp.o_x);
+  a.copied_w = at<char>(ws, sp.o_w);
+  a.part = at<float>(ws, sp.o_part);
+  return launch_linear(a, p, static_cast<hipStream_t>(stream)) == hipSuccess ? EXFOLD_OK : EXFOLD_ERR_DEVICE;
 }
 
 }  // extern "C"

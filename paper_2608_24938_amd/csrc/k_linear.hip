@@ -535,26 +535,35 @@ constexpr TileCost kTiles[] = {{kLinRing, 32, 64, 0.19f, 0.375f}, {kLinRing, 64,
                                {kLinRing, 64, 128, 0.36f, 1.16f}, {kLinRing, 128, 128, 0.52f, 2.33f},
                                {kLinWide, 256, 256, 1.6f, 0.f},   {kLinTile, 64, 128, 1.1f, 1.6f}};
 
+// Rows [0, rows_x) of x and [0, rows_w) of w, copied to rows of kp elements (whole pieces, zeros
+// behind K) at 16-byte alignment, a piece a thread at a time.
+template <typename E>
+__global__ __launch_bounds__(256) void linear_copy(const LinearArgs a, const E *x, const E *w, E *to_x, E *to_w,
+                                                  long long rows_x, long long rows_w, int kp) {
+  constexpr int EP = 16 / sizeof(E);
+  const int pieces = kp / EP;
+  const long long n = (rows_x + rows_w) * pieces;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+    const long long r = i / pieces;
+    const int k = (int)(i % pieces) * EP;
+    const bool of_x = r < rows_x;
+    const E *src = of_x ? x + r * a.ldx : w + (r - rows_x) * a.ldw;
+    E *dst = of_x ? to_x + r * kp : to_w + (r - rows_x) * kp;
+    *reinterpret_cast<u32x4 *>(dst + k) = load_piece(src + k, a.K - k);
+  }
+}
+
 // The tile and split of the least estimated time: rounds of tiles over the CUs, or the
 // weights' and rows' bytes from memory (about 4.8 TB/s) where those take longer, and for a
 // split its partial sums, written and read, and the launch that joins them.  The estimate
 // picks among kernels that all are right; it is within 20% of what they measured (600 x 2048
 // x 768 float32: 32 us on 32 x 64 tiles, 34 on 64 x 128, 57 on 128 x 128; 64 x 4096 x 4096
 // bf16: 13.4 us split in four, 15.3 not).
-LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int cu_count) {
-  LinearPlan p{};
-  p.ksplit = 1;
-  p.kc = K;
-  const bool bf16 = dtype == EXFOLD_BF16;
+static double plan_tiles(bool bf16, bool gated, bool vec, int M, int N, int K, int cu_count, LinearPlan &p) {
+  p = LinearPlan{};
+  p.vec = vec;
+  p.K = K;
   const long long wrows = (long long)N * (gated ? 2 : 1);
-  if (M <= kFewRows) {
-    p.kind = kLinFew;
-    p.bm = M <= 1 ? 1 : M <= 2 ? 2 : 4;
-    p.bn = wrows >= 16LL * cu_count ? 8 : 2;
-    const int cols = gated ? p.bn / 2 : p.bn;
-    p.grid = (N + cols - 1) / cols;
-    return p;
-  }
   const int stage = bf16 ? 64 : 32, stages = (K + stage - 1) / stage;
   const double memory = ((double)wrows * K + (double)M * K) * (bf16 ? 2 : 4) / 4.8e6;  // us
   double best = 0.0;
@@ -589,6 +598,42 @@ LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int
       p.grid = (int)(tiles * ksplit);
       p.shared_cu = p.grid > cu_count;
     }
+  }
+  return best;
+}
+
+LinearPlan plan_linear(int dtype, bool gated, bool vec_x, bool vec_w, int M, int N, int K, int cu_count) {
+  LinearPlan p{};
+  const bool bf16 = dtype == EXFOLD_BF16, whole = K % (bf16 ? 8 : 4) == 0;
+  const long long wrows = (long long)N * (gated ? 2 : 1);
+  if (M <= kFewRows) {
+    p.kind = kLinFew;
+    p.vec = vec_x && vec_w && whole;
+    p.K = K;
+    p.ksplit = 1;
+    p.bm = M <= 1 ? 1 : M <= 2 ? 2 : 4;
+    p.bn = wrows >= 16LL * cu_count ? 8 : 2;
+    const int cols = gated ? p.bn / 2 : p.bn;
+    p.grid = (N + cols - 1) / cols;
+    return p;
+  }
+  if (vec_x && vec_w && whole) {
+    plan_tiles(bf16, gated, true, M, N, K, cu_count, p);
+    return p;
+  }
+  // as the rows lie, or copied first: one launch more, the copies written and read.  Where K is no
+  // whole number of pieces both operands are copied, with zeros up to a whole stage; else only
+  // rows that start elsewhere are, and the length stays K for both.
+  const double direct = plan_tiles(bf16, gated, false, M, N, K, cu_count, p);
+  const int stage = bf16 ? 64 : 32, kp = whole ? K : (K + stage - 1) / stage * stage;
+  const bool px = !vec_x || !whole, pw = !vec_w || !whole;
+  LinearPlan q;
+  const double copied = plan_tiles(bf16, gated, true, M, N, kp, cu_count, q) + 3.0 +
+                        ((px ? M : 0) + (pw ? (double)wrows : 0.0)) * kp * (bf16 ? 2 : 4) * 2 / 4e6;
+  if (copied < direct) {
+    p = q;
+    p.copy_x = px;
+    p.copy_w = pw;
   }
   return p;
 }
@@ -628,13 +673,37 @@ static void launch_typed(const LinearArgs &a, const LinearPlan &p, hipStream_t s
   }
 }
 
-hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, bool vec, hipStream_t s) {
-  if (a.M <= 0) return hipSuccess;
+template <typename E>
+static void launch_copy(LinearArgs &a, const LinearPlan &p, hipStream_t s) {
+  const long long rows_x = p.copy_x ? a.M : 0, rows_w = p.copy_w ? (long long)a.N * (a.gated ? 2 : 1) : 0;
+  const long long n = (rows_x + rows_w) * (p.K / (16 / (int)sizeof(E)));
+  E *to_x = static_cast<E *>(a.copied_x), *to_w = static_cast<E *>(a.copied_w);
+  const long long blocks = (n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384;
+  linear_copy<E><<<(unsigned)blocks, 256, 0, s>>>(a, static_cast<const E *>(a.x), static_cast<const E *>(a.w), to_x,
+                                                         to_w, rows_x, rows_w, p.K);
+  if (p.copy_x) {
+    a.x = to_x;
+    a.ldx = p.K;
+  }
+  if (p.copy_w) {
+    a.w = to_w;
+    a.ldw = p.K;
+  }
+}
+
+hipError_t launch_linear(const LinearArgs &args, const LinearPlan &p, hipStream_t s) {
+  if (args.M <= 0) return hipSuccess;
+  LinearArgs a = args;
+  if (p.copy_x || p.copy_w) {
+    if (a.dtype == EXFOLD_BF16) launch_copy<bf16_t>(a, p, s);
+    else launch_copy<float>(a, p, s);
+    a.K = p.K;
+  }
   if (p.kind == kLinWide) return launch_linear_wide(a, p, s);
   auto typed = [&](auto e, auto gated) {
     using E = decltype(e);
     constexpr bool G = decltype(gated)::value;
-    vec ? launch_typed<E, G, true>(a, p, s) : launch_typed<E, G, false>(a, p, s);
+    p.vec ? launch_typed<E, G, true>(a, p, s) : launch_typed<E, G, false>(a, p, s);
   };
   auto by_gate = [&](auto e) { a.gated ? typed(e, std::true_type{}) : typed(e, std::false_type{}); };
   if (a.dtype == EXFOLD_BF16) by_gate(bf16_t{}); else by_gate(float{});

@@ -62,6 +62,7 @@ struct LinearArgs {
   long long ldx, ldw, ldr, ldy;
   int M, N, K, dtype, out_dtype, act;
   bool gated;
+  void *copied_x, *copied_w;  // [M, plan.K], [N or 2N, plan.K], where the plan copies
   float *part;  // [ksplit][M][linear_part_cols (gated: twice)] float32 partial sums, when split
 };
 // kLinFew: vector products of a few rows; kLinTile: MFMA tiles of four waves staged
@@ -75,12 +76,15 @@ struct LinearPlan {
   int kc;      // columns of a split (the last may hold fewer)
   int grid;
   bool shared_cu;  // more workgroups than CUs
+  bool vec;        // rows start on 16 bytes and hold whole 16-byte pieces
+  bool copy_x, copy_w;  // rows that do not are copied to rows of K elements first
+  int K;           // reduction length that the tiles run over (with copies: whole stages)
 };
-// vec: rows of x and w start on 16 bytes and K is a whole number of 16-byte pieces.
-LinearPlan plan_linear(int dtype, bool gated, bool vec, int M, int N, int K, int cu_count);
+// vec_x, vec_w: their rows start on 16 bytes.
+LinearPlan plan_linear(int dtype, bool gated, bool vec_x, bool vec_w, int M, int N, int K, int cu_count);
 // Columns of a row of partial sums (gated: the up columns follow, as many).
 __host__ __device__ inline int linear_part_cols(int N) { return (N + 3) / 4 * 4; }
-hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, bool vec, hipStream_t s);
+hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, hipStream_t s);
 hipError_t launch_linear_wide(const LinearArgs &a, const LinearPlan &p, hipStream_t s);  // k_gemm.hip
 
 // ---- permutation (k_permute.hip) ----

@@ -129,6 +129,30 @@ def test_strides_alignment_and_what_lies_between(M, N, K, gated, dtype, pad, shi
     assert (mark == 7.0).all()                                                          # nothing beside y's rows
 
 
+@pytest.mark.parametrize("M,N,K,gated", [(1, 96, 1000, False), (3, 40, 264, True), (20, 72, 200, False), (40, 256, 4104, False),
+                                         (300, 700, 136, True), (500, 1000, 2056, False), (2100, 1100, 192, False),
+                                         (300, 130, 333, False), (1100, 700, 2049, True)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("xpad,wpad,shift", [(64, 64, 0), (3, 64, 0), (64, 5, 1), (3, 3, 1)])
+def test_what_lies_behind_the_rows_is_not_used(M, N, K, gated, dtype, xpad, wpad, shift):
+    # NaN in front of the first row and in the gaps behind the rows of x, w and the residual: aligned rows
+    # (a whole number of 16-byte pieces or not), and either or both operands off alignment
+    if K * 2 % 16:
+        shift, xpad, wpad = 0, xpad + (-(K + xpad) % 8) * (xpad == 64), wpad + (-(K + wpad) % 8) * (wpad == 64)
+    g = torch.Generator().manual_seed(M)
+
+    def cut(rr, cc, pad, off, scale=1.0):
+        buf = torch.full((off + rr * (cc + pad),), float("nan"), dtype=dtype)
+        v = buf[off:].view(rr, cc + pad)
+        v[:, :cc] = torch.randn(rr, cc, generator=g) * scale
+        d = buf.to(DEV)
+        return d[off:].view(rr, cc + pad)[:, :cc]
+
+    x, w = cut(M, K, xpad, shift), cut(2 * N if gated else N, K, wpad, shift, 1.5 / K ** 0.5)
+    r = cut(M, N, 4, 2)
+    compare(X.linear(x, w, act="silu", gated=gated, residual=r), x, w, None, r, "silu", gated)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 256, 512), (12, 129, 2048), (100, 128, 4096), (1024, 512, 128)])
 def test_adds_onto_its_residual_in_place(M, N, K):
     for dtype in (torch.bfloat16, torch.float32):
