@@ -482,6 +482,25 @@ exfold_status exfold_linear_forward(const exfold_linear *linear, const void *x, 
                                     const void *residual, int64_t ldr, void *y, int64_t ldy, void *ws,
                                     size_t ws_bytes, void *stream);
 
+/* Kernel families of exfold_linear_forward (exfold_linear_plan). */
+enum {
+  EXFOLD_LINEAR_FEW = 0,   /* vector products of a few rows                              */
+  EXFOLD_LINEAR_TILE = 1,  /* MFMA tiles staged through registers (rows off alignment)   */
+  EXFOLD_LINEAR_RING = 2,  /* MFMA tiles through an LDS ring                             */
+  EXFOLD_LINEAR_WIDE = 3   /* 256 x 256 tiles (bf16)                                     */
+};
+
+/*
+ * Host-only query of the plan for M rows whose x starts rows on 16 bytes (x_aligned != 0)
+ * or not, on a device with `cu_count` compute units (the forward uses the device's count).
+ * out[8] = { kind, tile rows, weight rows of a tile, splits of the reduction, columns of a
+ * split, workgroups, x is copied first, w is copied first }.  Errors: those of the forward
+ * for `linear` and M; EXFOLD_ERR_NULL for out == NULL; EXFOLD_ERR_SHAPE for M < 1 or
+ * cu_count < 1.
+ */
+exfold_status exfold_linear_plan(const exfold_linear *linear, int64_t M, int32_t x_aligned, int32_t cu_count,
+                                 int32_t *out);
+
 #ifdef __cplusplus
 }
 #endif

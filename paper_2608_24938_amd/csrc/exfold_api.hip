@@ -800,9 +800,9 @@ exfold_status check_linear(const exfold_linear *L, int64_t M) {
 bool rows_aligned(const void *p, int64_t ld, int32_t dtype) {
   return !misaligned(p) && ld * (int64_t)element(dtype) % 16 == 0;
 }
-LinearPlan linear_plan(const exfold_linear *L, int64_t M, bool vec_x) {
+LinearPlan linear_plan(const exfold_linear *L, int64_t M, bool vec_x, int cus) {
   return plan_linear(L->dtype, L->gated != 0, vec_x, rows_aligned(L->w, L->ldw, L->dtype), (int)M, (int)L->n_out,
-                     (int)L->n_in, cu_count());
+                     (int)L->n_in, cus);
 }
 // Workspace of a call: copies of rows that are not aligned, then partial sums.
 struct LinearSpace {
@@ -868,8 +868,8 @@ exfold_status exfold_route_experts(const exfold_routing *r, const void *logits, 
 size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M) {
   if (check_linear(linear, M) != EXFOLD_OK || M == 0) return 0;
   // whichever rows of x the call brings
-  const size_t aligned = linear_space(linear, M, linear_plan(linear, M, true)).total;
-  const size_t any = linear_space(linear, M, linear_plan(linear, M, false)).total;
+  const size_t aligned = linear_space(linear, M, linear_plan(linear, M, true, cu_count())).total;
+  const size_t any = linear_space(linear, M, linear_plan(linear, M, false, cu_count())).total;
   return aligned > any ? aligned : any;
 }
 
@@ -884,7 +884,7 @@ exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64
   if (!x || !y) return EXFOLD_ERR_NULL;
   const int64_t esz = (int64_t)element(L->dtype), osz = (int64_t)element(L->out_dtype);
   if (unaligned_to(x, esz) || unaligned_to(y, osz) || unaligned_to(residual, osz)) return EXFOLD_ERR_ALIGN;
-  const LinearPlan p = linear_plan(L, M, rows_aligned(x, ldx, L->dtype));
+  const LinearPlan p = linear_plan(L, M, rows_aligned(x, ldx, L->dtype), cu_count());
   const LinearSpace sp = linear_space(L, M, p);
   const size_t need = sp.total;
   if (need > 0) {
@@ -920,6 +920,21 @@ exfold_status exfold_linear_forward(const exfold_linear *L, const void *x, int64
   a.copied_w = at<char>(ws, sp.o_w);
   a.part = at<float>(ws, sp.o_part);
   return launch_linear(a, p, static_cast<hipStream_t>(stream)) == hipSuccess ? EXFOLD_OK : EXFOLD_ERR_DEVICE;
+}
+
+static_assert(EXFOLD_LINEAR_FEW == kLinFew && EXFOLD_LINEAR_TILE == kLinTile && EXFOLD_LINEAR_RING == kLinRing &&
+                  EXFOLD_LINEAR_WIDE == kLinWide,
+              "the header's kernel families are the planner's");
+
+exfold_status exfold_linear_plan(const exfold_linear *L, int64_t M, int32_t x_aligned, int32_t cus, int32_t *out) {
+  exfold_status st = check_linear(L, M);
+  if (st != EXFOLD_OK) return st;
+  if (!out) return EXFOLD_ERR_NULL;
+  if (M < 1 || cus < 1) return EXFOLD_ERR_SHAPE;
+  const LinearPlan p = linear_plan(L, M, x_aligned != 0, cus);
+  const int32_t v[8] = {p.kind, p.bm, p.bn, p.ksplit, p.kc, p.grid, p.copy_x, p.copy_w};
+  for (int i = 0; i < 8; ++i) out[i] = v[i];
+  return EXFOLD_OK;
 }
 
 }  // extern "C"

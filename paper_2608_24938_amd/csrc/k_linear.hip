@@ -388,8 +388,8 @@ __global__ __launch_bounds__(256, BM == 128 && S > 2 ? 1 : 2) void linear_ring(c
 }
 
 // ---------------------------------------------------------------------------
-// Few rows (serving a token or four): the weights are read once and nothing is staged.  A
-// workgroup takes RW weight rows (gated: RW / 2 columns' gate and up rows) over the whole
+// Few rows (serving a token or four; a few times four where the weights are small): nothing is
+// staged.  A workgroup takes MT rows and RW weight rows (gated: RW / 2 columns' gate and up rows) over the whole
 // reduction, its 256 threads on consecutive 16-byte pieces of each (element loads where the
 // rows allow no pieces), two sweeps of loads in flight, products in float32 on the vector
 // units; the threads' sums are added by DPP within rows of 16 lanes and then in order through
@@ -421,11 +421,11 @@ template <typename E, int MT, int RW, bool GATED, bool VEC>
 __global__ __launch_bounds__(256) void linear_few(const LinearArgs a) {
   constexpr int EP = 16 / sizeof(E), U = 2, COLS = GATED ? RW / 2 : RW;
   __shared__ float part[16][RW * MT];
-  const int tid = threadIdx.x, n0 = blockIdx.x * COLS;
+  const int tid = threadIdx.x, n0 = blockIdx.x * COLS, m0 = blockIdx.y * MT;
   const E *x = static_cast<const E *>(a.x), *w = static_cast<const E *>(a.w);
   const E *xr[MT], *wr[RW];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) xr[m] = x + (long long)min(m, a.M - 1) * a.ldx;
+  for (int m = 0; m < MT; ++m) xr[m] = x + (long long)min(m0 + m, a.M - 1) * a.ldx;
 #pragma unroll
   for (int r = 0; r < RW; ++r) {
     const int n = min(n0 + (GATED ? r % COLS : r), a.N - 1);
@@ -478,7 +478,7 @@ __global__ __launch_bounds__(256) void linear_few(const LinearArgs a) {
   __syncthreads();
   if (tid >= COLS * MT) return;
   const int m = tid / COLS, c = tid % COLS, n = n0 + c;
-  if (m >= a.M || n >= a.N) return;
+  if (m0 + m >= a.M || n >= a.N) return;
   float z = 0.f, g = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -486,9 +486,9 @@ __global__ __launch_bounds__(256) void linear_few(const LinearArgs a) {
     if (GATED) g += part[i][m * RW + COLS + c];
   }
   if (sizeof(E) == 4 || a.out_dtype == EXFOLD_F32)
-    finish1<GATED, float>(a, m, n, z, g);
+    finish1<GATED, float>(a, m0 + m, n, z, g);
   else if constexpr (sizeof(E) == 2)
-    finish1<GATED, bf16_t>(a, m, n, z, g);
+    finish1<GATED, bf16_t>(a, m0 + m, n, z, g);
 }
 
 // Joins the split partial sums in order, four columns a thread, and finishes them.
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int kspli
 // ---------------------------------------------------------------------------
 // Planning and launch.
 // ---------------------------------------------------------------------------
-constexpr int kFewRows = 4;
+constexpr int kFewRows = 4, kFewMost = 64;  // rows: always, at most, on the vector units
 
 // Tiles and what a stage of one takes a CU that holds one workgroup of them or several in
 // turn (measured, microseconds).  bf16: the bytes of the stage at about 65 GB/s a CU, wide
@@ -587,7 +587,7 @@ static double plan_tiles(bool bf16, bool gated, bool vec, int M, int N, int K, i
       const int again = (M + t.bm - 1) / t.bm - 1;
       const double slow = memory * ((2 * wgs < 3 * cu_count ? 1.15 : 1.0) + 0.2 * (again < 3 ? again : 3));
       if (us < slow && memory > 10.0) us = slow + 0.05 * us;
-      if (ksplit > 1) us += 2.5 + ksplit * (double)M * wrows * 8 / 4e6;
+      if (ksplit > 1) us += 4.0 + ksplit * (double)M * wrows * 8 / 4e6;
       if (best > 0.0 && us >= best) continue;
       best = us;
       p.kind = t.kind;
@@ -606,20 +606,27 @@ LinearPlan plan_linear(int dtype, bool gated, bool vec_x, bool vec_w, int M, int
   LinearPlan p{};
   const bool bf16 = dtype == EXFOLD_BF16, whole = K % (bf16 ? 8 : 4) == 0;
   const long long wrows = (long long)N * (gated ? 2 : 1);
-  if (M <= kFewRows) {
+  // rows in groups of four on the vector units: the weights pass once a group, from the caches,
+  // at half the rate where their pieces lie across 16-byte borders (8 x 343 x 498 float32 at odd
+  // strides 10.4 -> 3.7 us, 16 x 128 x 2048 bf16 6.9 -> 3.3)
+  const int groups = (M + 3) / 4 * (vec_w ? 1 : 2);
+  const double few = groups * ((double)wrows * K * (bf16 ? 2 : 4) / 5e6 + (double)wrows * K * 4 / 30e6);  // us
+  auto take_few = [&] {
+    p = LinearPlan{};
     p.kind = kLinFew;
     p.vec = vec_x && vec_w && whole;
-    p.K = K;
+    p.K = p.kc = K;
     p.ksplit = 1;
     p.bm = M <= 1 ? 1 : M <= 2 ? 2 : 4;
     p.bn = wrows >= 16LL * cu_count ? 8 : 2;
     const int cols = gated ? p.bn / 2 : p.bn;
-    p.grid = (N + cols - 1) / cols;
+    p.grid = (N + cols - 1) / cols * ((M + p.bm - 1) / p.bm);
     return p;
-  }
+  };
+  if (M <= kFewRows) return take_few();
   if (vec_x && vec_w && whole) {
-    plan_tiles(bf16, gated, true, M, N, K, cu_count, p);
-    return p;
+    const double tiles = plan_tiles(bf16, gated, true, M, N, K, cu_count, p);
+    return M <= kFewMost && few < tiles ? take_few() : p;
   }
   // as the rows lie, or copied first: one launch more, the copies written and read.  Where K is no
   // whole number of pieces both operands are copied, with zeros up to a whole stage; else only
@@ -630,6 +637,7 @@ LinearPlan plan_linear(int dtype, bool gated, bool vec_x, bool vec_w, int M, int
   LinearPlan q;
   const double copied = plan_tiles(bf16, gated, true, M, N, kp, cu_count, q) + 3.0 +
                         ((px ? M : 0) + (pw ? (double)wrows : 0.0)) * kp * (bf16 ? 2 : 4) * 2 / 4e6;
+  if (M <= kFewMost && few < direct && few < copied) return take_few();
   if (copied < direct) {
     p = q;
     p.copy_x = px;
@@ -642,8 +650,10 @@ template <typename E, bool GATED, bool VEC>
 static void launch_few(const LinearArgs &a, const LinearPlan &p, hipStream_t s) {
   auto go = [&](auto mt) {
     constexpr int MT = decltype(mt)::value;
-    if (p.bn == 8) linear_few<E, MT, 8, GATED, VEC><<<p.grid, 256, 0, s>>>(a);
-    else linear_few<E, MT, 2, GATED, VEC><<<p.grid, 256, 0, s>>>(a);
+    const int y = (a.M + MT - 1) / MT;
+    const dim3 grid(p.grid / y, y);
+    if (p.bn == 8) linear_few<E, MT, 8, GATED, VEC><<<grid, 256, 0, s>>>(a);
+    else linear_few<E, MT, 2, GATED, VEC><<<grid, 256, 0, s>>>(a);
   };
   if (p.bm == 1) go(std::integral_constant<int, 1>{});
   else if (p.bm == 2) go(std::integral_constant<int, 2>{});

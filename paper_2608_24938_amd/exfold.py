@@ -33,7 +33,7 @@ EXPORTED = [
     "exfold_moe_execute", "exfold_calibrate_workspace_size", "exfold_calibrate_projectors",
     "exfold_calibrate_diagonal",
     "exfold_status_str", "exfold_gemm_plan",
-    "exfold_route_experts", "exfold_linear_workspace_size", "exfold_linear_forward",
+    "exfold_route_experts", "exfold_linear_workspace_size", "exfold_linear_forward", "exfold_linear_plan",
 ]
 
 
@@ -119,6 +119,7 @@ def lib() -> ctypes.CDLL:
             "exfold_route_experts": (i32, [vp, vp, i32, i64, i64, i64, i64, vp, vp, vp]),
             "exfold_linear_workspace_size": (sz, [vp, i64]),
             "exfold_linear_forward": (i32, [vp, vp, i64, i64, vp, i64, vp, i64, vp, sz, vp]),
+            "exfold_linear_plan": (i32, [vp, i64, i32, i32, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)

@@ -246,8 +246,8 @@ def test_empty_batch_and_binding_refusals():
         X.linear(x, w[:5], gated=True)
     with pytest.raises(X.ExfoldError):
         X.linear(x.float(), w.float(), out_dtype=torch.bfloat16)
-    long = torch.zeros(40, 8192, device=DEV, dtype=torch.bfloat16)
-    assert X.linear_workspace_size(long[:6], 40) > 255
+    long = torch.zeros(200, 8192, device=DEV, dtype=torch.bfloat16)
+    assert X.linear_workspace_size(long[:6], 200) > 255
     with pytest.raises(X.ExfoldError):
         X.linear(long, long[:6], workspace=torch.empty(255, dtype=torch.uint8, device=DEV))
     with pytest.raises(X.ExfoldError):

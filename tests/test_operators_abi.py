@@ -51,7 +51,7 @@ def test_route_no_tokens_is_a_no_op():
 XP, WP, BP, RP, YP, WS = F, 64 * F, 128 * F, 192 * F, 256 * F, 320 * F
 
 
-def linear(M=16, x=XP, ldx=None, res=None, ldr=0, y=YP, ldy=None, ws=WS, ws_bytes=None, lin=True, **kw):
+def linear(M=100, x=XP, ldx=None, res=None, ldr=0, y=YP, ldy=None, ws=WS, ws_bytes=None, lin=True, **kw):
     a = dict(n_in=4096, n_out=32, ldw=None, w=WP, bias=None, dtype=X.BF16, out_dtype=None, act=0, gated=0)
     a.update(kw)
     a["ldw"] = a["n_in"] if a["ldw"] is None else a["ldw"]
