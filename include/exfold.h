@@ -473,7 +473,8 @@ size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M);
  *   the workspace is EXFOLD_ERR_ARG.
  * Any sizes, strides and element-aligned pointers are valid; rows of x and w that start on
  * 16 bytes and hold a whole number of 16-byte pieces are read in 16-byte vectors and run
- * fastest.  M == 0 is a no-op; M <= 2^22, M * n_out <= 2^34 (else EXFOLD_ERR_SHAPE).
+ * fastest.  The order of a sum depends on the sizes, the types and which rows are so aligned,
+ * on nothing else.  M == 0 is a no-op; M <= 2^22, M * n_out <= 2^34 (else EXFOLD_ERR_SHAPE).
  * Errors: EXFOLD_ERR_DTYPE for an unknown dtype or a bf16 output of float32 inputs;
  * EXFOLD_ERR_ARG for an unknown activation or gate flag; EXFOLD_ERR_ALIGN for pointers not
  * aligned to their element.

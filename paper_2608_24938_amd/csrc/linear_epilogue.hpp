@@ -18,7 +18,8 @@ template <bool FAST> __device__ __forceinline__ float sigmoid_times(float z, flo
 template <int ACT, bool FAST> __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == EXFOLD_ACT_RELU) return z > 0.f ? z : 0.f;
   if constexpr (ACT == EXFOLD_ACT_SILU) return sigmoid_times<FAST>(z, z);
-  if constexpr (ACT == EXFOLD_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+  // z Phi(z), by the complementary function: 1 + erf would lose the lower tail
+  if constexpr (ACT == EXFOLD_ACT_GELU) return 0.5f * z * erfcf(z * -0.70710678f);
   // 0.5 z (1 + tanh u) = z / (1 + exp(-2 u)), u = sqrt(2 / pi) (z + 0.044715 z^3)
   if constexpr (ACT == EXFOLD_ACT_GELU_TANH)
     return sigmoid_times<FAST>(z, z * fmaf(0.07135481f * z, z, 1.59576912f));

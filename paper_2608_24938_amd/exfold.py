@@ -441,19 +441,20 @@ def _output(t, dtype, shape, name, device):
         raise ValueError(f"{name}: expected on {device}, got {t.device}")
 
 
-def _call_on(device, stream, fn, *args):
-    """Status of fn(*args, stream) with the tensors' device current, on the given stream or that device's current one."""
+def _call(device, fn, *args):
+    """Status of fn(*args, stream) with the tensors' device current, on that device's current stream."""
     index = device.index
-    if stream is None:
-        handle = _raw_stream(index)
-    elif stream.device == device:
-        handle = stream.cuda_stream
-    else:
-        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
     if index == torch.cuda.current_device():
-        return fn(*args, handle)
+        return fn(*args, _raw_stream(index))
     with torch.cuda.device(index):
-        return fn(*args, handle)
+        return fn(*args, _raw_stream(index))
+
+
+def _on_stream(stream, device):
+    """The context of a call on a given stream: what it allocates belongs to that stream too."""
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+    return torch.cuda.stream(stream)
 
 
 def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, keep_groups=1, group_top2=False,
@@ -464,10 +465,15 @@ def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, ke
     selection only.  groups, keep_groups: the selection is limited to the keep_groups of `groups` groups of
     consecutive experts with the largest value (their largest expert, or group_top2: the sum of the two
     largest).  renorm: the weights of a token's routes are divided by their sum; scale multiplies them.
-    A logit of -inf masks its expert (see exfold_routing in the header).  topk_ids/topk_w: optional outputs."""
+    A logit of -inf masks its expert (see exfold_routing in the header).  topk_ids/topk_w: optional outputs.
+    stream: as under torch.cuda.stream(stream)."""
     ld = _matrix(logits, "logits")
     T, N = logits.shape
     dev = logits.device
+    if stream is not None:
+        with _on_stream(stream, dev):
+            return route_experts(logits, top_k, score, select_bias, groups, keep_groups, group_top2, renorm, scale,
+                                 topk_ids, topk_w)
     bias = _vector(select_bias, N, "select_bias", dev)
     if score not in SCORE:
         raise ValueError(f"score: expected one of {sorted(SCORE)}, got {score!r}")
@@ -480,8 +486,8 @@ def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, ke
     else:
         _output(topk_w, torch.float32, (T, top_k), "topk_w", dev)
     r = _Routing(SCORE[score], 1 if group_top2 else 0, groups, keep_groups, 1 if renorm else 0, scale, bias)
-    status = _call_on(dev, stream, lib().exfold_route_experts, ctypes.byref(r), logits.data_ptr(), _DTYPE[logits.dtype],
-                      ld, T, N, top_k, topk_ids.data_ptr(), topk_w.data_ptr())
+    status = _call(dev, lib().exfold_route_experts, ctypes.byref(r), logits.data_ptr(), _DTYPE[logits.dtype], ld, T, N,
+                   top_k, topk_ids.data_ptr(), topk_w.data_ptr())
     if status != OK:
         raise ExfoldError(status, "exfold_route_experts")
     return topk_ids, topk_w
@@ -503,9 +509,13 @@ def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=No
     bfloat16, rows contiguous; bias [n_out] (gated [2 n_out]) float32; residual and y [M, n_out] of
     out_dtype (x's type unless given; float32 is always allowed).  y may be the residual (y += ...).
     act: "none", "relu", "silu", "gelu" or "gelu_tanh".  workspace: a tensor of at least
-    linear_workspace_size bytes; made here, where one is needed, unless given."""
+    linear_workspace_size bytes; made here, where one is needed, unless given.  stream: as under
+    torch.cuda.stream(stream)."""
     ldx = _matrix(x, "x")
     dev, dtype = x.device, x.dtype
+    if stream is not None:
+        with _on_stream(stream, dev):
+            return linear(x, w, bias, act, gated, residual, out_dtype, y, workspace)
     M, K = x.shape
     ldw = _matrix(w, "w", dtype, None, dev)
     rows, kw = w.shape
@@ -530,16 +540,18 @@ def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=No
         y, ldy = torch.empty(M, n_out, dtype=out_dtype, device=dev), n_out
     else:
         ldy = _matrix(y, "y", out_dtype, (M, n_out), dev)
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise ValueError(f"workspace: expected a contiguous tensor on {dev}, got one on {workspace.device}")
     p = ctypes.byref(_Linear(K, n_out, ldw, w.data_ptr(), b, _DTYPE[dtype], _DTYPE[out_dtype], ACT[act], 1 if gated else 0))
     L = lib()
     args = (p, x.data_ptr(), ldx, M, res, ldr, y.data_ptr(), ldy)
     if workspace is None:  # most small products need none: ask for its size only when the call does
-        status = _call_on(dev, stream, L.exfold_linear_forward, *args, None, 0)
+        status = _call(dev, L.exfold_linear_forward, *args, None, 0)
         if status == ERR_WORKSPACE:
-            workspace = _workspace(L.exfold_linear_workspace_size(p, M), dev, stream)
+            workspace = _workspace(L.exfold_linear_workspace_size(p, M), dev)
     if workspace is not None:
-        status = _call_on(dev, stream, L.exfold_linear_forward, *args, workspace.data_ptr(),
-                          workspace.numel() * workspace.element_size())
+        status = _call(dev, L.exfold_linear_forward, *args, workspace.data_ptr(),
+                       workspace.numel() * workspace.element_size())
     if status != OK:
         raise ExfoldError(status, "exfold_linear_forward")
     return y

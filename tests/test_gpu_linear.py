@@ -244,6 +244,9 @@ def test_empty_batch_and_binding_refusals():
             X.linear(xb, wb)
     with pytest.raises(ValueError):
         X.linear(x, w[:5], gated=True)
+    for ws in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1 << 11, 1 << 10, device=DEV).t()):
+        with pytest.raises(ValueError):
+            X.linear(x, w, workspace=ws)
     with pytest.raises(X.ExfoldError):
         X.linear(x.float(), w.float(), out_dtype=torch.bfloat16)
     long = torch.zeros(200, 8192, device=DEV, dtype=torch.bfloat16)
