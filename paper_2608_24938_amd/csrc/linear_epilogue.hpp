@@ -15,11 +15,27 @@ template <bool FAST> __device__ __forceinline__ float sigmoid_times(float z, flo
   else
     return z / (1.0f + expf(-u));
 }
+// Phi(z) within 1e-5 of its value on all of the lower tail: Phi(-|z|) = exp(-z^2 / 2) times half the
+// scaled complementary error function of |z| / sqrt(2), which is smooth in t = 1 / (1 + |z| /
+// (2 sqrt(2))): a polynomial of degree 7 without constant term, fitted to least relative error
+// over |z| < 13.  (The library's function takes about 100 instructions: 777 x 1408 outputs of
+// 64-long rows 8.7 us, 5.4 without an activation.)
+__device__ __forceinline__ float normal_cdf(float z) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.35355339f, fabsf(z), 1.0f));
+  float p = fmaf(0.0445633493f, t, -0.179994732f);
+  p = fmaf(p, t, 0.196891531f);
+  p = fmaf(p, t, 0.0173283778f);
+  p = fmaf(p, t, 0.141360044f);
+  p = fmaf(p, t, 0.138676807f);
+  p = fmaf(p, t, 0.141174048f);
+  const float q = p * t * __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+  return z < 0.f ? q : 1.0f - q;
+}
 template <int ACT, bool FAST> __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == EXFOLD_ACT_RELU) return z > 0.f ? z : 0.f;
   if constexpr (ACT == EXFOLD_ACT_SILU) return sigmoid_times<FAST>(z, z);
   // z Phi(z), by the complementary function: 1 + erf would lose the lower tail
-  if constexpr (ACT == EXFOLD_ACT_GELU) return 0.5f * z * erfcf(z * -0.70710678f);
+  if constexpr (ACT == EXFOLD_ACT_GELU) return FAST ? z * normal_cdf(z) : 0.5f * z * erfcf(z * -0.70710678f);
   // 0.5 z (1 + tanh u) = z / (1 + exp(-2 u)), u = sqrt(2 / pi) (z + 0.044715 z^3)
   if constexpr (ACT == EXFOLD_ACT_GELU_TANH)
     return sigmoid_times<FAST>(z, z * fmaf(0.07135481f * z, z, 1.59576912f));
