@@ -29,6 +29,18 @@ template <typename E> __device__ __forceinline__ void mma32(const u32x4 &a, cons
 // LDS slot (16-byte units) of piece q of tile row r (8 pieces a row).
 __device__ __forceinline__ int piece_at(int r, int q) { return r * 8 + (q ^ ((r ^ (r >> 1)) & 7)); }
 
+// Tile of logical id L: panels of kPanel m-tiles, m-tile fastest in a panel, then the n-tiles, then
+// the panels, then the splits, so that an XCD's consecutive ids share rows and weights (8192 x
+// 1024 x 4096 83.6 -> 78.4 us against all m-tiles first).
+constexpr int kPanel = 8;
+__device__ __forceinline__ void tile_of(int L, int mts, int nts, int &mt, int &nt, int &ks) {
+  ks = L / (mts * nts);
+  L -= ks * mts * nts;
+  const int panel = L / (kPanel * nts), in = L - panel * kPanel * nts, pm = min(kPanel, mts - panel * kPanel);
+  nt = in / pm;
+  mt = panel * kPanel + in - nt * pm;
+}
+
 // Sums of a wave's TM x TN tiles to the outputs, or to the partial sums of split ks.  Register r
 // of tile (i, j): row row0 + arow(i) + lane % 32, tile column brow(j) + 8 (r / 4) + 4 (lane / 32)
 // + r % 4 (the weights are the MFMA's first operand): runs of four columns.
@@ -105,8 +117,8 @@ __global__ __launch_bounds__(256, 2) void linear_tile(const LinearArgs a, const 
   __shared__ __attribute__((aligned(16))) u32x4 smem[2][(BM + BN) * 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
   const int mts = (a.M + BM - 1) / BM, nts = (a.N + COLS - 1) / COLS;
-  const int L = xcd_remap(blockIdx.x, mts * nts * p.ksplit);
-  const int mt = L % mts, nt = L / mts % nts, ks = L / mts / nts;
+  int mt, nt, ks;
+  tile_of(xcd_remap(blockIdx.x, mts * nts * p.ksplit), mts, nts, mt, nt, ks);
   const int k0 = ks * p.kc, k1 = min(a.K, k0 + p.kc), kq = (tid & 7) * EP;
   const E *sa[PA], *sb[PB];
 #pragma unroll
@@ -232,8 +244,8 @@ __global__ __launch_bounds__(256, BM == 128 && S > 2 ? 1 : 2) void linear_ring(c
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = KW ? 0 : wave >> 1, wn = KW ? 0 : wave & 1;
   const int mts = (a.M + BM - 1) / BM, nts = (a.N + COLS - 1) / COLS;
-  const int L = xcd_remap(blockIdx.x, mts * nts * p.ksplit);
-  const int mt = L % mts, nt = L / mts % nts, ks = L / mts / nts;
+  int mt, nt, ks;
+  tile_of(xcd_remap(blockIdx.x, mts * nts * p.ksplit), mts, nts, mt, nt, ks);
   const int k0 = ks * p.kc, k1 = min(a.K, k0 + p.kc), stages = (k1 - k0 + KS - 1) / KS;
 
   // 1 KiB block i of this wave: rows 8 (4 i + wave) .. + 7 of the stage, x rows first
