@@ -514,7 +514,7 @@ __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int kspli
   const int n = (int)(i % quads_n) * 4;
   const float *row = a.part + m * ld + n;
   f32x4 zs = {0.f, 0.f, 0.f, 0.f}, us = zs;
-#pragma unroll 4
+#pragma unroll 8
   for (int s = 0; s < ksplit; ++s) {
     zs += *reinterpret_cast<const f32x4 *>(row + s * split);
     if (GATED) us += *reinterpret_cast<const f32x4 *>(row + s * split + np);
