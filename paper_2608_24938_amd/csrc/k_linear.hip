@@ -10,13 +10,10 @@ namespace exfold {
 // ---------------------------------------------------------------------------
 // Tiles of BM rows x BN weight rows (gated: BN / 2 gate rows and the BN / 2 up rows of the
 // same columns), four waves of 32x32 MFMA tiles.  A stage is 128 bytes of the reduction (64
-// bf16 or 32 float32 columns) of every row, staged through registers into one of two LDS
-// buffers, its 16-byte pieces swizzled so that a fragment read spreads over the banks; the
-// next stage's loads fly during the MFMAs.  A lane's piece of a row feeds one 32x32x16 bf16
-// MFMA or four 32x32x2 float32 ones (any assignment of columns to steps is a valid order).
-// VEC: rows start on 16 bytes and K is a whole number of pieces; else element loads, 64 (32)
-// consecutive ones a wave.  Rows past the ends re-read the last one and are not stored;
-// columns past K are zero.
+// bf16 or 32 float32 columns) of every row in LDS, its 16-byte pieces swizzled so that a
+// fragment read spreads over the banks.  A lane's piece of a row feeds one 32x32x16 bf16 MFMA
+// or four 32x32x2 float32 ones (any assignment of columns to steps is a valid order).  Rows
+// past the ends re-read the last one and are not stored; columns past K are zero.
 // ---------------------------------------------------------------------------
 template <typename E> constexpr int mma_steps() { return sizeof(E) == 2 ? 1 : 4; }
 template <typename E> __device__ __forceinline__ void mma32(const u32x4 &a, const u32x4 &b, int e, f32x16 &c) {
@@ -108,6 +105,8 @@ template <typename E> __device__ __forceinline__ u32x4 load_piece(const E *p, in
   return v;
 }
 
+// Rows at any alignment: the stages pass through registers into one of two LDS buffers, loaded in
+// 16-byte pieces that may lie across 16-byte borders (elements at a row's end), two stages ahead.
 template <typename E, int BM, int BN, bool GATED>
 __global__ __launch_bounds__(256, 2) void linear_tile(const LinearArgs a, const LinearPlan p) {
   constexpr int EP = 16 / sizeof(E), KS = 8 * EP;
@@ -401,11 +400,11 @@ __global__ __launch_bounds__(256, BM == 128 && S > 2 ? 1 : 2) void linear_ring(c
 
 // ---------------------------------------------------------------------------
 // Few rows (serving a token or four; a few times four where the weights are small): nothing is
-// staged.  A workgroup takes MT rows and RW weight rows (gated: RW / 2 columns' gate and up rows) over the whole
-// reduction, its 256 threads on consecutive 16-byte pieces of each (element loads where the
-// rows allow no pieces), two sweeps of loads in flight, products in float32 on the vector
-// units; the threads' sums are added by DPP within rows of 16 lanes and then in order through
-// LDS.
+// staged.  A workgroup takes MT rows and RW weight rows (gated: RW / 2 columns' gate and up
+// rows) over the whole reduction, its 256 threads on consecutive 16-byte pieces of each (VEC:
+// the rows start on 16 bytes and hold whole pieces), two sweeps of loads in flight, products
+// in float32 on the vector units; the threads' sums are added by DPP within rows of 16 lanes
+// and then in order through LDS.  One token, 2 x 1408 weight rows of 4096: 6.0 us, 3.9 TB/s.
 // ---------------------------------------------------------------------------
 // Elements of a 16-byte piece as float32.
 template <typename E> __device__ __forceinline__ void unpack_piece(const u32x4 &v, float (&f)[16 / sizeof(E)]) {

@@ -442,7 +442,7 @@ def _output(t, dtype, shape, name, device):
 
 
 def _call(device, fn, *args):
-    """Status of fn(*args, stream) with the tensors' device current, on that device's current stream."""
+    """fn(*args, stream) with the tensors' device current, on that device's current stream."""
     index = device.index
     if index == torch.cuda.current_device():
         return fn(*args, _raw_stream(index))
@@ -499,7 +499,7 @@ def linear_workspace_size(w, rows, gated=False) -> int:
     n_out = w.shape[0] // 2 if gated else w.shape[0]
     code = _DTYPE[w.dtype]
     ls = _Linear(w.shape[1], n_out, ldw, w.data_ptr(), None, code, code, 0, 1 if gated else 0)
-    return lib().exfold_linear_workspace_size(ctypes.byref(ls), rows)
+    return _call(w.device, lambda _: lib().exfold_linear_workspace_size(ctypes.byref(ls), rows))
 
 
 def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=None, y=None, workspace=None, stream=None):
@@ -548,7 +548,7 @@ def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=No
     if workspace is None:  # most small products need none: ask for its size only when the call does
         status = _call(dev, L.exfold_linear_forward, *args, None, 0)
         if status == ERR_WORKSPACE:
-            workspace = _workspace(L.exfold_linear_workspace_size(p, M), dev)
+            workspace = _workspace(_call(dev, lambda _: L.exfold_linear_workspace_size(p, M)), dev)
     if workspace is not None:
         status = _call(dev, L.exfold_linear_forward, *args, workspace.data_ptr(),
                        workspace.numel() * workspace.element_size())
