@@ -1581,32 +1581,33 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void linear_wide(const LinearAr
     case 3: wide_tile_mma<false, 3>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
     default: wide_tile_mma<false, 2>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
   }
-  // runs of four columns of a row: 4 j + g
-  constexpr int NQ = GATED ? 4 : 8;
-  auto col = [&](int q) { return nt * COLS + wide_col<false>(wn, 0, q >> 2) + 8 * (q & 3) + 4 * (lane >> 5); };
-  f32x4 bz[NQ], bu[NQ];
-  bias_quads<GATED>(a, col, bz, bu);
-  auto finish = [&](auto out) {
-    with_act(a.act, [&](auto act) {
+  // the sums through LDS in two halves of 128 rows (the ring is free after the main loop)
+  constexpr int PITCH = kWideBN + 4;  // floats of a row
+  static_assert(kWide / 2 * PITCH * 4 <= kWideSmemElems * 2, "a half fits the ring");
+  float *red = reinterpret_cast<float *>(smem);
 #pragma unroll
-      for (int i = 0; i < kWideTM; ++i) {
-        const int ml = wide_row<false>(wm, i) + (lane & 31);
-        if (ml >= valid) continue;
-        finish_row<decltype(act)::value, GATED, decltype(out)>(
-            a, mt * kWide + ml, bz, bu, col, [&](int q, f32x4 &z, f32x4 &u) __attribute__((always_inline)) {
+  for (int h = 0; h < 2; ++h) {
+    if (h * (kWide / 2) >= valid) break;
+    if (h) __syncthreads();
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                z[e] = acc[i][GATED ? 0 : q >> 2][4 * (q & 3) + e];
-                if constexpr (GATED) u[e] = acc[i][1][4 * q + e];
-              }
-            });
-      }
-    });
-  };
-  if (a.out_dtype == EXFOLD_F32)
-    finish(float{});
-  else
-    finish(bf16_t{});
+    for (int ib = 0; ib < 2; ++ib) {
+      const int i = 2 * h + ib;
+#pragma unroll
+      for (int j = 0; j < kWideTN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x16 &c = acc[i][j];
+          *reinterpret_cast<f32x4 *>(red + (wide_row<true>(wm, i) + (lane & 31)) * PITCH + wide_col<false>(wn, i, j) + 8 * g +
+                                     4 * (lane >> 5)) = f32x4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
+        }
+    }
+    __syncthreads();
+    const int row0 = mt * kWide + h * (kWide / 2), rows = min(kWide / 2, valid - h * (kWide / 2));
+    if (a.out_dtype == EXFOLD_F32)
+      finish_tile<GATED, float, COLS, PITCH, 1, 64 * kWideWaves>(a, red, 0, row0, nt * COLS, rows);
+    else
+      finish_tile<GATED, bf16_t, COLS, PITCH, 1, 64 * kWideWaves>(a, red, 0, row0, nt * COLS, rows);
+  }
 }
 
 hipError_t launch_linear_wide(const LinearArgs &a, const LinearPlan &p, hipStream_t s) {

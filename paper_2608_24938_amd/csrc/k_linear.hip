@@ -38,54 +38,31 @@ __device__ __forceinline__ void tile_of(int L, int mts, int nts, int &mt, int &n
   mt = panel * kPanel + in - nt * pm;
 }
 
-// Sums of a wave's TM x TN tiles to the outputs, or to the partial sums of split ks.  Register r
-// of tile (i, j): row row0 + arow(i) + lane % 32, tile column brow(j) + 8 (r / 4) + 4 (lane / 32)
-// + r % 4 (the weights are the MFMA's first operand): runs of four columns.
-template <typename E, int TM, int TN, int COLS, bool GATED, typename RowA, typename RowB>
-__device__ __forceinline__ void tile_epilogue(const LinearArgs &a, const LinearPlan &p, int row0, int nt, int ks, int lane,
-                                              const f32x16 (&acc)[TM][TN], const RowA &arow, const RowB &brow) {
-  auto quad = [&](int i, int q) __attribute__((always_inline)) {  // run q of row block i
-    const f32x16 &c = acc[i][q >> 2];
-    return f32x4{c[4 * (q & 3)], c[4 * (q & 3) + 1], c[4 * (q & 3) + 2], c[4 * (q & 3) + 3]};
-  };
-  auto at = [&](int q) { return brow(q >> 2) + 8 * (q & 3) + 4 * (lane >> 5); };  // its tile column
-  if (p.ksplit > 1) {
-    const int np = linear_part_cols(a.N);
+// A wave's TM x TN tiles of sums into LDS, row-major: register r of tile (i, j) is row arow(i) +
+// lane % 32, column brow(j) + 8 (r / 4) + 4 (lane / 32) + r % 4 (the weights are the MFMA's first
+// operand): runs of four columns.
+template <int PITCH, int TM, int TN, typename RowA, typename RowB>
+__device__ __forceinline__ void sums_to_lds(float *red, const f32x16 (&acc)[TM][TN], int lane, const RowA &arow,
+                                            const RowB &brow) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int m = row0 + arow(i) + (lane & 31);
-      if (m >= a.M) continue;
-      float *row = a.part + ((long long)ks * a.M + m) * np * (GATED ? 2 : 1);
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int q = 0; q < 4 * TN; ++q) {
-        const int c = at(q), n = nt * COLS + (GATED ? c & (COLS - 1) : c);
-        if (n < a.N) *reinterpret_cast<f32x4 *>(row + (GATED && c >= COLS ? np : 0) + n) = quad(i, q);
-      }
-    }
-    return;
-  }
-  constexpr int NQ = GATED ? 2 * TN : 4 * TN;
-  auto col = [&](int q) { return nt * COLS + at(q); };
-  f32x4 bz[NQ], bu[NQ];
-  bias_quads<GATED>(a, col, bz, bu);
-  auto finish = [&](auto out) {
-    with_act(a.act, [&](auto act) {
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const int m = row0 + arow(i) + (lane & 31);
-        if (m >= a.M) continue;
-        finish_row<decltype(act)::value, GATED, decltype(out)>(
-            a, m, bz, bu, col, [&](int q, f32x4 &z, f32x4 &u) __attribute__((always_inline)) {
-              z = quad(i, q);
-              if constexpr (GATED) u = quad(i, q + NQ);
-            });
-      }
-    });
-  };
-  if (sizeof(E) == 4 || a.out_dtype == EXFOLD_F32)
-    finish(float{});
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4 *>(red + (arow(i) + (lane & 31)) * PITCH + brow(j) + 8 * g + 4 * (lane >> 5)) =
+            f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+}
+// Outputs or partial sums of a tile from its sums in LDS (all threads, after a barrier).
+template <typename E, int BM, int COLS, int PITCH, int COPIES, bool GATED>
+__device__ __forceinline__ void tile_out(const LinearArgs &a, const LinearPlan &p, const float *red, int mt, int nt, int ks) {
+  const int rows = min(BM, a.M - mt * BM);
+  if (p.ksplit > 1)
+    store_partial<GATED, COLS, PITCH, COPIES, 256>(a, ks, red, BM * PITCH, mt * BM, nt * COLS, rows);
+  else if (sizeof(E) == 4 || a.out_dtype == EXFOLD_F32)
+    finish_tile<GATED, float, COLS, PITCH, COPIES, 256>(a, red, BM * PITCH, mt * BM, nt * COLS, rows);
   else if constexpr (sizeof(E) == 2)
-    finish(bf16_t{});
+    finish_tile<GATED, bf16_t, COLS, PITCH, COPIES, 256>(a, red, BM * PITCH, mt * BM, nt * COLS, rows);
 }
 
 // A 16-byte piece of a row at any element alignment, `left` elements of which exist (the rest 0).
@@ -113,6 +90,8 @@ __global__ __launch_bounds__(256, 2) void linear_tile(const LinearArgs a, const 
   constexpr int TM = BM / 64, TN = BN / 64, COLS = GATED ? BN / 2 : BN;
   constexpr int PA = BM * 8 / 256, PB = BN * 8 / 256;  // pieces a thread
   static_assert(!GATED || TN % 2 == 0, "a wave holds the gate and the up columns");
+  constexpr int PITCH = BN + 4;  // floats of a row of sums
+  static_assert(BM * PITCH * 4 <= 2 * (BM + BN) * 128, "the sums fit the stages");
   __shared__ __attribute__((aligned(16))) u32x4 smem[2][(BM + BN) * 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
   const int mts = (a.M + BM - 1) / BM, nts = (a.N + COLS - 1) / COLS;
@@ -193,7 +172,12 @@ __global__ __launch_bounds__(256, 2) void linear_tile(const LinearArgs a, const 
     stage(0, ra0, rb0);
     __syncthreads();
   }
-  tile_epilogue<E, TM, TN, COLS, GATED>(a, p, mt * BM, nt, ks, lane, acc, arow, brow);
+  // the last stage's barrier is behind every wave's reads
+  __syncthreads();
+  float *red = reinterpret_cast<float *>(&smem[0][0]);
+  sums_to_lds<PITCH>(red, acc, lane, arow, brow);
+  __syncthreads();
+  tile_out<E, BM, COLS, PITCH, 1, GATED>(a, p, red, mt, nt, ks);
 }
 
 // ---------------------------------------------------------------------------
@@ -223,14 +207,6 @@ template <bool ONCE> __device__ __forceinline__ void ring_load(const char *g, ui
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(lds) : "memory", "m0");
 }
 
-// Sum of the four waves' values at red (wave-major, BM rows of PITCH floats each), in wave order.
-template <int BM, int PITCH> __device__ __forceinline__ f32x4 kw_sum(const float *red) {
-  f32x4 v = *reinterpret_cast<const f32x4 *>(red);
-#pragma unroll
-  for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4 *>(red + w * BM * PITCH);
-  return v;
-}
-
 template <typename E, int BM, int BN, int S, bool KW, bool GATED, bool ONCE>
 __global__ __launch_bounds__(256, BM == 128 && S > 2 ? 1 : 2) void linear_ring(const LinearArgs a, const LinearPlan p) {
   constexpr int EP = 16 / sizeof(E), KS = 8 * EP, ROWS = BM + BN, NB = ROWS / 32;
@@ -238,7 +214,7 @@ __global__ __launch_bounds__(256, BM == 128 && S > 2 ? 1 : 2) void linear_ring(c
   constexpr int COLS = GATED ? BN / 2 : BN;
   static_assert(!GATED || TN % 2 == 0, "a wave holds the gate and the up columns");
   constexpr int PITCH = BN + 4;  // floats of a row of the waves' sums
-  constexpr int RING = S * ROWS * 8, RED = KW ? 4 * BM * PITCH / 4 : 0;
+  constexpr int RING = S * ROWS * 8, RED = (KW ? 4 : 1) * BM * PITCH / 4;
   __shared__ __attribute__((aligned(1024))) u32x4 smem[RING > RED ? RING : RED];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = KW ? 0 : wave >> 1, wn = KW ? 0 : wave & 1;
@@ -351,51 +327,10 @@ __global__ __launch_bounds__(256, BM == 128 && S > 2 ? 1 : 2) void linear_ring(c
   // no load into the ring is left, and every wave has read it
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
 
-  if constexpr (!KW) {
-    tile_epilogue<E, TM, TN, COLS, GATED>(a, p, mt * BM, nt, ks, lane, acc, arow, brow);
-  } else {
-    float *red = reinterpret_cast<float *>(smem);
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4 *>(red + (wave * BM + i * 32 + (lane & 31)) * PITCH + j * 32 + 8 * g + 4 * (lane >> 5)) =
-              f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-    __syncthreads();
-    if (p.ksplit > 1) {
-      const int np = linear_part_cols(a.N);
-      float *part = a.part + (long long)ks * a.M * np * (GATED ? 2 : 1);
-      for (int i = tid; i < BM * BN / 4; i += 256) {
-        const int ml = i / (BN / 4), c = i % (BN / 4) * 4, m = mt * BM + ml, n = nt * COLS + (GATED ? c & (COLS - 1) : c);
-        if (m < a.M && n < a.N)
-          *reinterpret_cast<f32x4 *>(part + (long long)m * np * (GATED ? 2 : 1) + (GATED && c >= COLS ? np : 0) + n) =
-              kw_sum<BM, PITCH>(red + ml * PITCH + c);
-      }
-      return;
-    }
-    // run i of this thread: row tid / (COLS / 4) + i of as many rows as 256 threads cover
-    constexpr int QN = COLS / 4, RN = 256 / QN;
-    const int n = nt * COLS + tid % QN * 4;
-    auto col = [&](int) { return n; };
-    f32x4 bz[1], bu[1];
-    bias_quads<GATED>(a, col, bz, bu);
-    auto finish = [&](auto out) {
-      with_act(a.act, [&](auto act) {
-        for (int ml = tid / QN; ml < BM && mt * BM + ml < a.M; ml += RN)
-          finish_row<decltype(act)::value, GATED, decltype(out)>(
-              a, mt * BM + ml, bz, bu, col, [&](int, f32x4 &z, f32x4 &u) __attribute__((always_inline)) {
-                z = kw_sum<BM, PITCH>(red + ml * PITCH + tid % QN * 4);
-                if constexpr (GATED) u = kw_sum<BM, PITCH>(red + ml * PITCH + COLS + tid % QN * 4);
-              });
-      });
-    };
-    if (sizeof(E) == 4 || a.out_dtype == EXFOLD_F32)
-      finish(float{});
-    else if constexpr (sizeof(E) == 2)
-      finish(bf16_t{});
-  }
+  float *red = reinterpret_cast<float *>(smem);
+  sums_to_lds<PITCH>(red + (KW ? wave * BM * PITCH : 0), acc, lane, arow, brow);
+  __syncthreads();
+  tile_out<E, BM, COLS, PITCH, KW ? 4 : 1, GATED>(a, p, red, mt, nt, ks);
 }
 
 // ---------------------------------------------------------------------------
@@ -518,15 +453,10 @@ __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int kspli
     zs += *reinterpret_cast<const f32x4 *>(row + s * split);
     if (GATED) us += *reinterpret_cast<const f32x4 *>(row + s * split + np);
   }
-  auto col = [&](int) { return n; };
-  f32x4 bz[1], bu[1];
-  bias_quads<GATED>(a, col, bz, bu);
-  with_act(a.act, [&](auto act) {
-    finish_row<decltype(act)::value, GATED, O>(a, m, bz, bu, col, [&](int, f32x4 &z, f32x4 &u) {
-      z = zs;
-      u = us;
-    });
-  });
+  f32x4 bz, bu, r = {0.f, 0.f, 0.f, 0.f};
+  bias_quad<GATED>(a, n, bz, bu);
+  if (a.res) r = load_quad(static_cast<const O *>(a.res) + m * a.ldr, n, a.N);
+  with_act(a.act, [&](auto act) { finish_quad<decltype(act)::value, GATED, O>(a, m, n, zs, us, bz, bu, r); });
 }
 
 // ---------------------------------------------------------------------------
@@ -534,17 +464,17 @@ __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int kspli
 // ---------------------------------------------------------------------------
 constexpr int kFewRows = 4, kFewMost = 64;  // rows: always, at most, on the vector units
 
-// Tiles and what a stage of one takes a CU that holds one workgroup of them or several in
-// turn (measured, microseconds).  bf16: the bytes of the stage at about 65 GB/s a CU, wide
-// tiles by their MFMAs; float32: the MFMAs.  The register-staged tiles wait for their loads,
-// and two workgroups a CU overlap.
+// Tiles, what a stage of one takes a CU that holds one workgroup of them or several in turn,
+// and what a tile takes besides (first loads, epilogue); measured, microseconds.  bf16: the
+// bytes of the stage at about 65 GB/s a CU, wide tiles by their MFMAs; float32: the MFMAs.  The
+// register-staged tiles wait for their loads, and two workgroups a CU overlap.
 struct TileCost {
   int kind, bm, bn;
-  float bf16, f32;
+  float bf16, f32, once;
 };
-constexpr TileCost kTiles[] = {{kLinRing, 32, 64, 0.19f, 0.375f}, {kLinRing, 64, 64, 0.24f, 0.66f},
-                               {kLinRing, 64, 128, 0.36f, 1.16f}, {kLinRing, 128, 128, 0.52f, 2.33f},
-                               {kLinWide, 256, 256, 1.6f, 0.f},   {kLinTile, 64, 128, 1.1f, 1.6f}};
+constexpr TileCost kTiles[] = {{kLinRing, 32, 64, 0.19f, 0.35f, 1.6f},  {kLinRing, 64, 64, 0.24f, 0.66f, 2.3f},
+                               {kLinRing, 64, 128, 0.36f, 1.16f, 3.2f}, {kLinRing, 128, 128, 0.52f, 2.33f, 7.f},
+                               {kLinWide, 256, 256, 1.5f, 0.f, 10.f},   {kLinTile, 64, 128, 1.1f, 1.6f, 3.2f}};
 
 // Rows [0, rows_x) of x and [0, rows_w) of w, copied to rows of kp elements (whole pieces, zeros
 // behind K) at 16-byte alignment, a piece a thread at a time.
@@ -593,7 +523,7 @@ static double plan_tiles(bool bf16, bool gated, bool vec, int M, int N, int K, i
       }
       const int per = (int)((stages + split - 1) / split), ksplit = (stages + per - 1) / per;
       const long long wgs = tiles * ksplit, round = t.kind == kLinTile ? 2 * cu_count : cu_count;
-      double us = (double)((wgs + round - 1) / round) * per * (bf16 ? t.bf16 : t.f32);
+      double us = (double)((wgs + round - 1) / round) * (per * (bf16 ? t.bf16 : t.f32) + t.once);
       // few streams are slower, and tiles of rows drift apart, so their weights come again
       const int again = (M + t.bm - 1) / t.bm - 1;
       const double slow = memory * ((2 * wgs < 3 * cu_count ? 1.15 : 1.0) + 0.2 * (again < 3 ? again : 3));

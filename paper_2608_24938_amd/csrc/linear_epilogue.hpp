@@ -79,52 +79,91 @@ template <typename T> __device__ __forceinline__ f32x4 load_quad(const T *row, i
   return v;
 }
 
-// Outputs of NQ runs of four columns of row m: run i is columns col(i) .. + 3 (N or more: none)
-// with sums sum(i, z, u) (u: up sums of a gated product).  The row's residual is loaded before
-// its first output is stored: y may be the residual, so the compiler keeps the loads in front
-// of the stores only as they are written here, and one wait covers them all (a run at a time,
-// each waited for its own: 600 x 2048 float32 outputs of 768-long rows 38 us).
-// bz, bu: the bias of the runs (bias_quads).
-template <int ACT, bool GATED, typename O, int NQ, typename Col, typename Sum>
-__device__ __forceinline__ void finish_row(const LinearArgs &a, long long m, const f32x4 (&bz)[NQ], const f32x4 (&bu)[NQ],
-                                           const Col &col, const Sum &sum) {
-  f32x4 rv[NQ];
-  const O *r = static_cast<const O *>(a.res) + m * a.ldr;
-  O *y = static_cast<O *>(a.y) + m * a.ldy;
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    rv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (a.res && col(i) < a.N) rv[i] = load_quad(r, col(i), a.N);
-  }
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int n = col(i);
-    if (n >= a.N) continue;
-    f32x4 z, u;
-    sum(i, z, u);
-    z += bz[i];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = activate<ACT, sizeof(O) == 2>(z[e]);
-    if constexpr (GATED) z *= u + bu[i];
-    z += rv[i];
-    if (n + 4 <= a.N) {
-      store_quad(y + n, z);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (n + e < a.N) y[n + e] = store_cvt<O>(z[e]);
-    }
+// Bias of columns n .. n + 3 (gated: bz of the gate, bu of the up columns).
+template <bool GATED> __device__ __forceinline__ void bias_quad(const LinearArgs &a, int n, f32x4 &bz, f32x4 &bu) {
+  bz = bu = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (a.bias && n < a.N) {
+    bz = load_quad(a.bias, n, a.N);
+    if (GATED) bu = load_quad(a.bias + a.N, n, a.N);
   }
 }
-template <bool GATED, int NQ, typename Col>
-__device__ __forceinline__ void bias_quads(const LinearArgs &a, const Col &col, f32x4 (&bz)[NQ], f32x4 (&bu)[NQ]) {
+// Outputs (m, n) .. (m, n + 3), n < N, from their sums z (gated: gate sums z, up sums u), the bias
+// and the residual r.
+template <int ACT, bool GATED, typename O>
+__device__ __forceinline__ void finish_quad(const LinearArgs &a, long long m, int n, f32x4 z, const f32x4 &u,
+                                            const f32x4 &bz, const f32x4 &bu, const f32x4 &r) {
+  z += bz;
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    bz[i] = bu[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (a.bias && col(i) < a.N) {
-      bz[i] = load_quad(a.bias, col(i), a.N);
-      if (GATED) bu[i] = load_quad(a.bias + a.N, col(i), a.N);
+  for (int e = 0; e < 4; ++e) z[e] = activate<ACT, sizeof(O) == 2>(z[e]);
+  if constexpr (GATED) z *= u + bu;
+  z += r;
+  O *y = static_cast<O *>(a.y) + m * a.ldy + n;
+  if (n + 4 <= a.N) {
+    store_quad(y, z);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (n + e < a.N) y[e] = store_cvt<O>(z[e]);
+  }
+}
+
+// The tiles' sums go through LDS, and a loop of a few rows a thread finishes them in row-major
+// order: whole lines of r and y instead of 16-byte pieces of 32 rows, and a loop's instructions
+// instead of a whole tile's.  Against finishing each wave's registers where they are: 777 x 1411 x
+// 1003 with residual 22.8 -> 20.9 us, 1237 x 2816 x 4096 gated 44.6 -> 42.8, float32 600 x 2048 x
+// 768 29.3 -> 28.6, 8192 x 28672 x 4096 gated 1492 -> 1487 to 1512.
+//
+// `rows` rows of `COLS` outputs (gated: COLS gate sums, then COLS up sums) at red, PITCH floats a
+// row, COPIES of them `copy` floats apart to be added in order; outputs (row0, n0) on.  The
+// residual of a thread's rows of one turn is loaded before their outputs are stored (y may be
+// the residual, so the compiler keeps the order written here).
+template <int COPIES> __device__ __forceinline__ f32x4 lds_sum(const float *red, int copy) {
+  f32x4 v = *reinterpret_cast<const f32x4 *>(red);
+#pragma unroll
+  for (int w = 1; w < COPIES; ++w) v += *reinterpret_cast<const f32x4 *>(red + w * copy);
+  return v;
+}
+template <bool GATED, typename O, int COLS, int PITCH, int COPIES, int THREADS>
+__device__ __forceinline__ void finish_tile(const LinearArgs &a, const float *red, int copy, long long row0, int n0, int rows) {
+  constexpr int QN = COLS / 4, RN = THREADS / QN, U = 4;
+  const int q = threadIdx.x % QN * 4, n = n0 + q;
+  if (n >= a.N) return;
+  f32x4 bz, bu;
+  bias_quad<GATED>(a, n, bz, bu);
+  const O *res = static_cast<const O *>(a.res);
+  with_act(a.act, [&](auto act) {
+#pragma unroll 1
+    for (int m0 = threadIdx.x / QN; m0 < rows; m0 += RN * U) {
+      f32x4 r[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        r[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int m = m0 + i * RN;
+        if (res && m < rows) r[i] = load_quad(res + (row0 + m) * a.ldr, n, a.N);
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int m = m0 + i * RN;
+        if (m >= rows) break;
+        const float *at = red + m * PITCH + q;
+        finish_quad<decltype(act)::value, GATED, O>(a, row0 + m, n, lds_sum<COPIES>(at, copy),
+                                                    GATED ? lds_sum<COPIES>(at + COLS, copy) : f32x4{0.f, 0.f, 0.f, 0.f},
+                                                    bz, bu, r[i]);
+      }
     }
+  });
+}
+// The same sums as partial sums of split ks (a.part).
+template <bool GATED, int COLS, int PITCH, int COPIES, int THREADS>
+__device__ __forceinline__ void store_partial(const LinearArgs &a, int ks, const float *red, int copy, int row0, int n0,
+                                              int rows) {
+  constexpr int H = GATED ? 2 : 1, QN = COLS * H / 4;
+  const int np = linear_part_cols(a.N);
+  for (int i = threadIdx.x; i < rows * QN; i += THREADS) {
+    const int m = i / QN, c = i % QN * 4, n = n0 + (GATED ? c & (COLS - 1) : c);
+    if (n < a.N)
+      *reinterpret_cast<f32x4 *>(a.part + ((long long)ks * a.M + row0 + m) * np * H + (GATED && c >= COLS ? np : 0) + n) =
+          lds_sum<COPIES>(red + m * PITCH + c, copy);
   }
 }
 
