@@ -462,7 +462,7 @@ __global__ __launch_bounds__(256) void linear_join(const LinearArgs a, int kspli
 // ---------------------------------------------------------------------------
 // Planning and launch.
 // ---------------------------------------------------------------------------
-constexpr int kFewRows = 4, kFewMost = 64;  // rows: always, at most, on the vector units
+constexpr int kFewRows = 4, kFewMost = 64;  // rows: always, at most (of more than 8 weight rows), on the vector units
 
 // Tiles, what a stage of one takes a CU that holds one workgroup of them or several in turn,
 // and what a tile takes besides (first loads, epilogue); measured, microseconds.  bf16: the
@@ -547,27 +547,32 @@ LinearPlan plan_linear(int dtype, bool gated, bool vec_x, bool vec_w, int M, int
   LinearPlan p{};
   const bool bf16 = dtype == EXFOLD_BF16, whole = K % (bf16 ? 8 : 4) == 0;
   const long long wrows = (long long)N * (gated ? 2 : 1);
-  // rows in groups of four on the vector units: the weights pass once a group, from the caches,
-  // at half the rate where their pieces lie across 16-byte borders (8 x 343 x 498 float32 at odd
-  // strides 10.4 -> 3.7 us, 16 x 128 x 2048 bf16 6.9 -> 3.3)
-  const int groups = (M + 3) / 4 * (vec_w ? 1 : 2);
-  const double few = groups * ((double)wrows * K * (bf16 ? 2 : 4) / 5e6 + (double)wrows * K * 4 / 30e6);  // us
+  // Rows in groups of four on the vector units: the weights pass once a group and the rows once
+  // a block of weight rows, mostly from the caches, at half the rate where pieces lie across
+  // 16-byte borders; a round of workgroups takes its loads' latency whatever they read (8 x 343 x
+  // 498 float32 at odd strides 3.7 us, 10.4 copied to tiles; 16 x 128 x 2048 bf16 3.3 and 6.9; 10
+  // x 2 x 4464 x 120 float32, 3348 workgroups, 15.0).
+  const int few_rows = M <= 1 ? 1 : M <= 2 ? 2 : 4, few_cols = (wrows >= 16LL * cu_count ? 8 : 2) / (gated ? 2 : 1);
+  const int groups = (M + few_rows - 1) / few_rows, blocks = (N + few_cols - 1) / few_cols, esz = bf16 ? 2 : 4;
+  const bool few_fits = M <= kFewMost || (wrows <= 8 && M <= (1 << 16));
+  const double few = ((double)groups * wrows * K / 5e6 + (double)blocks * M * K / 10e6) * esz * (vec_w && whole ? 1 : 2) +
+                     (double)groups * wrows * K * 4 / 30e6 +
+                     2.5 * (double)(((long long)groups * blocks - 1) / ((few_cols > 2 ? 3 : 6) * (long long)cu_count) + 1);  // us
   auto take_few = [&] {
     p = LinearPlan{};
     p.kind = kLinFew;
     p.vec = vec_x && vec_w && whole;
     p.K = p.kc = K;
     p.ksplit = 1;
-    p.bm = M <= 1 ? 1 : M <= 2 ? 2 : 4;
-    p.bn = wrows >= 16LL * cu_count ? 8 : 2;
-    const int cols = gated ? p.bn / 2 : p.bn;
-    p.grid = (N + cols - 1) / cols * ((M + p.bm - 1) / p.bm);
+    p.bm = few_rows;
+    p.bn = few_cols * (gated ? 2 : 1);
+    p.grid = blocks * groups;
     return p;
   };
   if (M <= kFewRows) return take_few();
   if (vec_x && vec_w && whole) {
     const double tiles = plan_tiles(bf16, gated, true, M, N, K, cu_count, p);
-    return M <= kFewMost && few < tiles ? take_few() : p;
+    return few_fits && few < tiles ? take_few() : p;
   }
   // as the rows lie, or copied first: one launch more, the copies written and read.  Where K is no
   // whole number of pieces both operands are copied, with zeros up to a whole stage; else only
@@ -578,7 +583,7 @@ LinearPlan plan_linear(int dtype, bool gated, bool vec_x, bool vec_w, int M, int
   LinearPlan q;
   const double copied = plan_tiles(bf16, gated, true, M, N, kp, cu_count, q) + 3.0 +
                         ((px ? M : 0) + (pw ? (double)wrows : 0.0)) * kp * (bf16 ? 2 : 4) * 2 / 4e6;
-  if (M <= kFewMost && few < direct && few < copied) return take_few();
+  if (few_fits && few < direct && few < copied) return take_few();
   if (copied < direct) {
     p = q;
     p.copy_x = px;

@@ -100,6 +100,8 @@ def test_activations_over_their_range(act, M, dtype):
     (1237, 1408, 512, True, torch.bfloat16, torch.bfloat16), (1500, 768, 2048, False, torch.bfloat16, torch.bfloat16),
     (2049, 2050, 256, False, torch.bfloat16, torch.bfloat16), (1111, 700, 129, True, torch.bfloat16, torch.bfloat16),
     (3, 600, 4100, False, torch.float32, torch.float32), (700, 515, 768, False, torch.float32, torch.float32),
+    (5000, 1, 2056, False, torch.bfloat16, torch.float32), (333, 3, 1003, True, torch.bfloat16, torch.bfloat16),
+    (66000, 2, 40, False, torch.float32, torch.float32), (1030, 7, 515, False, torch.bfloat16, torch.bfloat16),
     (2000, 256, 260, True, torch.float32, torch.float32), (40, 64, 9000, False, torch.float32, torch.float32),
 ])
 def test_large(M, N, K, gated, dtype, out_dtype):
@@ -250,9 +252,9 @@ def test_empty_batch_and_binding_refusals():
     with pytest.raises(X.ExfoldError):
         X.linear(x.float(), w.float(), out_dtype=torch.bfloat16)
     long = torch.zeros(200, 8192, device=DEV, dtype=torch.bfloat16)
-    assert X.linear_workspace_size(long[:6], 200) > 255
+    assert X.linear_workspace_size(long[:64], 200) > 255
     with pytest.raises(X.ExfoldError):
-        X.linear(long, long[:6], workspace=torch.empty(255, dtype=torch.uint8, device=DEV))
+        X.linear(long, long[:64], workspace=torch.empty(255, dtype=torch.uint8, device=DEV))
     with pytest.raises(X.ExfoldError):
         X.linear(x, w, y=torch.zeros(1, 6, device=DEV, dtype=torch.bfloat16).expand(4, 6))
 

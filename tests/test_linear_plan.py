@@ -21,6 +21,7 @@ def plan(m, n, k, dtype=X.BF16, gated=False, x_aligned=True, ldw=None, cu=256):
 
 @pytest.mark.parametrize("args,kw,kind", [
     ((1, 128, 2048), {}, FEW), ((4, 28672, 4096), {}, FEW), ((1, 7, 13), {}, FEW),
+    ((5000, 1, 2056), {}, FEW), ((16, 128, 2048), {}, FEW), ((66000, 2, 2048), {}, RING),
     ((32, 4096, 14336), {}, RING), ((64, 28672, 4096), {}, RING), ((600, 2048, 768), dict(dtype=X.F32), RING),
     ((1237, 1408, 4096), dict(gated=True), RING), ((8192, 14336, 4096), dict(gated=True), WIDE),
     ((8192, 8192, 8192), {}, WIDE), ((8192, 8192, 8192), dict(dtype=X.F32), RING),
