@@ -1581,7 +1581,9 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void linear_wide(const LinearAr
     case 3: wide_tile_mma<false, 3>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
     default: wide_tile_mma<false, 2>(row_a, row_b, 0, a.K / kWideBK, smem, acc); break;
   }
-  // the sums through LDS in two halves of 128 rows (the ring is free after the main loop)
+  // the sums through LDS in two halves of 128 rows (the ring is free after the main loop); from
+  // the registers 8192 x 28672 x 4096 gated took 1488 us against 1498, but 8192 x 8192 x 1024 with
+  // a float32 residual 278 against 229 and 8192 x 8192 x 512 with gelu 137 against 116
   constexpr int PITCH = kWideBN + 4;  // floats of a row
   static_assert(kWide / 2 * PITCH * 4 <= kWideSmemElems * 2, "a half fits the ring");
   float *red = reinterpret_cast<float *>(smem);

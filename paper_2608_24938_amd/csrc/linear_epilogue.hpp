@@ -111,7 +111,7 @@ __device__ __forceinline__ void finish_quad(const LinearArgs &a, long long m, in
 // order: whole lines of r and y instead of 16-byte pieces of 32 rows, and a loop's instructions
 // instead of a whole tile's.  Against finishing each wave's registers where they are: 777 x 1411 x
 // 1003 with residual 22.8 -> 20.9 us, 1237 x 2816 x 4096 gated 44.6 -> 42.8, float32 600 x 2048 x
-// 768 29.3 -> 28.6, 8192 x 28672 x 4096 gated 1492 -> 1487 to 1512.
+// 768 29.3 -> 28.6.
 //
 // `rows` rows of `COLS` outputs (gated: COLS gate sums, then COLS up sums) at red, PITCH floats a
 // row, COPIES of them `copy` floats apart to be added in order; outputs (row0, n0) on.  The
