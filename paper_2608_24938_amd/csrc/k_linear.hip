@@ -497,9 +497,9 @@ __global__ __launch_bounds__(256) void linear_copy(const LinearArgs a, const E *
 // The tile and split of the least estimated time: rounds of tiles over the CUs, or the
 // weights' and rows' bytes from memory (about 4.8 TB/s) where those take longer, and for a
 // split its partial sums, written and read, and the launch that joins them.  The estimate
-// picks among kernels that all are right; it is within 20% of what they measured (600 x 2048
-// x 768 float32: 32 us on 32 x 64 tiles, 34 on 64 x 128, 57 on 128 x 128; 64 x 4096 x 4096
-// bf16: 13.4 us split in four, 15.3 not).
+// picks among kernels that all are right (600 x 2048 x 768 float32: 29 us on 32 x 64 tiles, 33
+// on 64 x 128 and 34 on 128 x 128; 777 x 1408 x 1024 bf16: 15.5, 13.4, 19.7, and 12.4 on 64 x
+// 64; 64 x 4096 x 4096 bf16: 13.4 us split in four, 15.3 not).
 static double plan_tiles(bool bf16, bool gated, bool vec, int M, int N, int K, int cu_count, LinearPlan &p) {
   p = LinearPlan{};
   p.vec = vec;
