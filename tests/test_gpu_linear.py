@@ -187,7 +187,8 @@ def test_infinities_and_nan_stay_in_their_rows(M, N, K):
 
 
 @pytest.mark.parametrize("M,N,K,gated", [(1, 1408, 4096, True), (32, 512, 14336, False), (200, 256, 4096, False),
-                                         (1024, 512, 1024, True)])
+                                         (1024, 512, 1024, True), (1100, 700, 2049, True), (40, 300, 513, False),
+                                         (3000, 4096, 256, False)])
 def test_identical_calls_and_graph_replays_are_bitwise_equal(M, N, K, gated):
     x, w, b, r = data(M, N, K, torch.bfloat16, gated, True, True, torch.bfloat16)
     y = torch.empty_like(r)
@@ -310,3 +311,23 @@ def test_block_of_linear_routing_folding_and_experts(T, phase, budget):
     assert per_token_rel_l2(from_dev(routed), ref).max() <= 2e-2
     compare(hid, x, sgu, None, None, "silu", True)
     compare(y, hid, sdn, None, routed, "none", False)
+
+
+@pytest.mark.parametrize("M,N,K", [(70000, 24, 64), (70000, 3, 40), (66000, 256, 128), (70000, 24, 63)])
+def test_row_offsets_past_32_bits(M, N, K):
+    # rows of x, the residual and y 33000 elements apart (the last row starts past 2^31 elements): the last
+    # rows against the same rows on their own
+    ld = 33000 if K % 8 == 0 else 32999
+    buf = torch.empty(M * ld, dtype=torch.bfloat16, device=DEV)
+    wide = buf.view(M, ld)
+    g = torch.Generator(device=DEV).manual_seed(M)
+    x, r, y = wide[:, :K], wide[:, 1000:1000 + N], wide[:, 2000:2000 + N]
+    x.copy_(torch.randn(M, K, generator=g, device=DEV))
+    r.copy_(torch.randn(M, N, generator=g, device=DEV))
+    wide[:, 2000 + N:2001 + N] = 7.0
+    w = (torch.randn(N, K, generator=g, device=DEV) / K ** 0.5).bfloat16()
+    X.linear(x, w, act="silu", residual=r, y=y)
+    sync()
+    for rows in (slice(0, 50), slice(M // 2, M // 2 + 50), slice(M - 50, M)):
+        compare(y[rows].contiguous(), x[rows].contiguous(), w, None, r[rows].contiguous(), "silu", False)
+    assert (wide[:, 2000 + N] == 7.0).all()

@@ -138,3 +138,43 @@ def test_binding_refusals():
         X.route_experts(l, 9)
     with pytest.raises(X.ExfoldError):
         X.route_experts(torch.zeros(1, 8, device=DEV).expand(4, 8), 2)      # rows on one another
+
+
+def test_row_offsets_past_32_bits():
+    T, N, ld = 70000, 96, 33000
+    buf = torch.empty(T * ld, dtype=torch.bfloat16, device=DEV).view(T, ld)
+    logits = buf[:, 8:8 + N]
+    logits.copy_(torch.randn(T, N, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV))
+    kw = dict(score="sigmoid", groups=6, keep_groups=3, group_top2=True)
+    ids, w = X.route_experts(logits, 5, **kw)
+    sync()
+    for rows in (slice(0, 40), slice(T - 40, T)):
+        rid, rw = P.route_experts(logits[rows].float().cpu().numpy(), 5, **kw)
+        np.testing.assert_array_equal(ids[rows].cpu().numpy(), rid)
+        np.testing.assert_allclose(w[rows].cpu().numpy().astype(np.float64), rw, rtol=RTOL, atol=ATOL)
+
+
+@pytest.mark.parametrize("T", [1, 500])
+def test_graph_replays_match_eager(T):
+    kw = dict(score="sigmoid", groups=8, keep_groups=4, group_top2=True, scale=2.5,
+              select_bias=(0.1 * torch.randn(128, generator=torch.Generator().manual_seed(1))).to(DEV))
+    logits = make(T, 128, torch.float32, 1, "plain").to(DEV)
+    ids = torch.empty(T, 8, dtype=torch.int32, device=DEV)
+    w = torch.empty(T, 8, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        X.route_experts(logits, 8, topk_ids=ids, topk_w=w, **kw)
+    torch.cuda.current_stream().wait_stream(side)
+    sync()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        X.route_experts(logits, 8, topk_ids=ids, topk_w=w, **kw)
+    for rep in range(4):
+        logits.copy_(make(T, 128, torch.float32, 10 + rep, "ties" if rep % 2 else "masked"))
+        ref = X.route_experts(logits, 8, **kw)
+        ids.fill_(-1)
+        w.fill_(-1.0)
+        graph.replay()
+        sync()
+        assert torch.equal(ids, ref[0]) and torch.equal(w, ref[1]), f"replay {rep}"
