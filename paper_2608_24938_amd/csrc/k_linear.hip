@@ -621,6 +621,7 @@ static void launch_typed(const LinearArgs &a, const LinearPlan &p, hipStream_t s
     else if (p.bm == 32) linear_ring<E, 32, 64, S32, true, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.bn == 64 && once) linear_ring<E, 64, 64, 4, true, GATED, true><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.bn == 64) linear_ring<E, 64, 64, 4, true, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+    else if (p.bm == 64 && p.kc <= 2 * 128 / (int)sizeof(E)) linear_ring<E, 64, 128, 2, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.bm == 64) linear_ring<E, 64, 128, 3, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.shared_cu) linear_ring<E, 128, 128, 2, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else linear_ring<E, 128, 128, 4, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
