@@ -614,7 +614,8 @@ static void launch_typed(const LinearArgs &a, const LinearPlan &p, hipStream_t s
     // Buffers: as many stages as two workgroups a CU leave room for where the loads are waited
     // for, few where several workgroups a CU cover each other: float32 on 32 x 64 tiles (600 x
     // 2048 x 768: three 29.0 us, six 32.2), and 128 x 128 tiles that are more than the CUs
-    // (2048 x 4096 x 4096: two 76.2 us, four 87.6; 128 x 28672 x 4096, 224 tiles: 74.6, 63.6).
+    // (2048 x 4096 x 4096: two 76.2 us, four 87.6; 128 x 28672 x 4096, 224 tiles: 74.6, 63.6), and
+    // reductions of two stages on 64 x 128 tiles (5498 x 7744 x 64: two 74.5 us, three 101.6).
     constexpr int S32 = sizeof(E) == 4 ? 3 : 6;
     const bool once = a.M <= p.bm;
     if (p.bm == 32 && once) linear_ring<E, 32, 64, S32, true, GATED, true><<<p.grid, 256, 0, s>>>(a, p);
