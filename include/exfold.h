@@ -435,8 +435,8 @@ exfold_status exfold_route_experts(const exfold_routing *routing, const void *lo
  *   gated:  y = act(x W_g^T + b_g) * (x W_u^T + b_u) + r,  W_g the first n_out rows of
  *           w and W_u the next n_out (the layout of exfold_layer.ws_gate_up).
  * Sums in float32, one rounding to out_dtype.
- *   ACT_SILU: z / (1 + e^-z); ACT_GELU: z Phi(z); ACT_GELU_TANH: z (1 + tanh(sqrt(2/pi)
- *   (z + 0.044715 z^3))) / 2.
+ *   ACT_RELU: max(z, 0); ACT_SILU: z / (1 + e^-z); ACT_GELU: z Phi(z); ACT_GELU_TANH: z (1 +
+ *   tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2.  A z of NaN stays NaN in each of them.
  */
 enum {
   EXFOLD_ACT_NONE = 0,

@@ -32,7 +32,7 @@ __device__ __forceinline__ float normal_cdf(float z) {
   return z < 0.f ? q : 1.0f - q;
 }
 template <int ACT, bool FAST> __device__ __forceinline__ float activate(float z) {
-  if constexpr (ACT == EXFOLD_ACT_RELU) return z > 0.f ? z : 0.f;
+  if constexpr (ACT == EXFOLD_ACT_RELU) return z <= 0.f ? 0.f : z;  // NaN stays NaN
   if constexpr (ACT == EXFOLD_ACT_SILU) return sigmoid_times<FAST>(z, z);
   // z Phi(z), by the complementary function: 1 + erf would lose the lower tail
   if constexpr (ACT == EXFOLD_ACT_GELU) return FAST ? z * normal_cdf(z) : 0.5f * z * erfcf(z * -0.70710678f);
