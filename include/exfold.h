@@ -99,7 +99,8 @@ enum {
  *   CONFIDENCE: c_s = clip(1 - min_t L[s, t], 0, 1); the target receives
  *               w_s c_s S[s, t] and w_s (1 - c_s) is spread over the retained
  *               routes in proportion to their router weights (Appendix F,
- *               Eq. dsv4_confidence, with L as the source-relative residual).
+ *               Eq. dsv4_confidence, with L as the source-relative residual);
+ *               nothing is spread where those weights sum to 0.
  * Safeguard arithmetic is float64, rounded once to float32 (see the oracle's
  * fold_prefill_safeguarded for the order of operations). */
 enum { EXFOLD_FOLD_LOSS_CAP = 1, EXFOLD_FOLD_RENORM = 2, EXFOLD_FOLD_CONFIDENCE = 4 };

@@ -279,7 +279,7 @@ def fold_prefill_safeguarded(ids, w, keep, S, L, loss_cap=None, renorm: bool = F
       minimum-loss target t* receives w_s c_s S[s, t*] and the remainder
       w_s (1 - c_s) is spread over the retained routes in proportion to their
       router weights, w_t / sum of retained w (R23; L is the source-relative
-      residual of Eq. dsv4_confidence).
+      residual of Eq. dsv4_confidence); nothing is spread where that sum is 0.
     * renorm: after folding, the retained weights are scaled by
       (sum of all K router weights) / (sum of the folded weights), when that
       sum is positive (R24).
@@ -321,7 +321,7 @@ def fold_prefill_safeguarded(ids, w, keep, S, L, loss_cap=None, renorm: bool = F
             if confidence:
                 c = min(1.0, max(0.0, 1.0 - float(L[s, ids[i, q_t]])))
             acc[q_t] = acc[q_t] + (ww[i, j] * c) * float(S[s, ids[i, q_t]])
-            if confidence:
+            if confidence and w_ret != 0.0:
                 rest = ww[i, j] * (1.0 - c)
                 for q in ret:
                     acc[q] = acc[q] + rest * (ww[i, q] / w_ret)

@@ -573,11 +573,12 @@ __device__ __forceinline__ void route_token_wave(const RouteArgs &a, int t, int 
   }
   // Coalesce onto each retained route, omitted routes in route order: the
   // target's share, then (confidence split) the spread w_s (1 - c_s) w_t / W_ret.
+  // W_ret of 0 (a token without a live expert: all routes weigh 0): nothing is spread.
   double w_ret = 0.0;
   if (conf)
     for (int j = 0; j < K; ++j)
       if ((kmask >> j) & 1ull) w_ret = __dadd_rn(w_ret, (double)readlane_f32(my_w, j));
-  const double share = (conf && kept) ? __ddiv_rn((double)my_w, w_ret) : 0.0;
+  const double share = (conf && kept && w_ret != 0.0) ? __ddiv_rn((double)my_w, w_ret) : 0.0;
   double acc = (double)my_w;
   for (int j = 0; j < K; ++j) {
     const int tl = (int)readlane_u32((uint32_t)tgt_lane, j);
