@@ -438,6 +438,7 @@ exfold_status exfold_route_experts(const exfold_routing *routing, const void *lo
  * Sums in float32, one rounding to out_dtype.
  *   ACT_RELU: max(z, 0); ACT_SILU: z / (1 + e^-z); ACT_GELU: z Phi(z); ACT_GELU_TANH: z (1 +
  *   tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2.  A z of NaN stays NaN in each of them.
+ *   They are evaluated in float32, off by at most 2^-20 of |z|.
  */
 enum {
   EXFOLD_ACT_NONE = 0,
