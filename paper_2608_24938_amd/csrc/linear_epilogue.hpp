@@ -38,7 +38,7 @@ __device__ __forceinline__ float gelu_few_ulps(float z) {
   return fmaf(-m, q, __builtin_elementwise_maximum(z, 0.0f));  // NaN stays NaN
 }
 template <int ACT, bool FAST> __device__ __forceinline__ float activate(float z) {
-  if constexpr (ACT == EXFOLD_ACT_RELU) return z <= 0.f ? 0.f : z;  // NaN stays NaN
+  if constexpr (ACT == EXFOLD_ACT_RELU) return __builtin_elementwise_maximum(z, 0.0f);  // NaN stays NaN
   if constexpr (ACT == EXFOLD_ACT_SILU) return sigmoid_times<FAST>(z, z);
   // z Phi(z), by the complementary function: 1 + erf would lose the lower tail
   if constexpr (ACT == EXFOLD_ACT_GELU) return FAST ? gelu_few_ulps(z) : 0.5f * z * erfcf(z * -0.70710678f);
