@@ -460,11 +460,14 @@ typedef struct exfold_linear {
   int32_t gated;      /* 0 or 1                                                    */
 } exfold_linear;
 
-/* Bytes of workspace exfold_linear_forward needs for M rows: 0 where it needs none (ws may
- * then be NULL), and on invalid input.  A call without one (NULL, 0 bytes) that needs it
- * returns EXFOLD_ERR_WORKSPACE.  It holds partial sums and copies of unaligned rows during
- * the call, so calls that overlap in time (other streams, graphs replayed together) need
- * workspaces of their own. */
+/* Bytes of workspace exfold_linear_forward needs for exactly M rows, this w and the
+ * current device, whatever the alignment of x: 0 where none is needed (ws may then be NULL),
+ * and on invalid input.  Fewer rows may need more, since their reduction is split
+ * further: a workspace for several batch sizes is as large as the largest of their sizes.  Rows
+ * of x that start on 16 bytes may need less, down to none.  A call without a workspace (NULL, 0
+ * bytes) that needs one returns EXFOLD_ERR_WORKSPACE.  It holds partial sums and copies of
+ * unaligned rows during the call, so calls that overlap in time (other streams, graphs replayed
+ * together) need workspaces of their own. */
 size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M);
 
 /*
@@ -475,8 +478,9 @@ size_t exfold_linear_workspace_size(const exfold_linear *linear, int64_t M);
  *   the workspace is EXFOLD_ERR_ARG.
  * Any sizes, strides and element-aligned pointers are valid; rows of x and w that start on
  * 16 bytes and hold a whole number of 16-byte pieces are read in 16-byte vectors and run
- * fastest.  The order of a sum depends on the sizes, the types and which rows are so aligned,
- * on nothing else.  M == 0 is a no-op; M <= 2^22, M * n_out <= 2^34 (else EXFOLD_ERR_SHAPE).
+ * fastest.  The order of a sum depends on the sizes, the types, which rows are so aligned and
+ * the device's number of compute units, on nothing else.  M == 0 is a no-op; M <= 2^22,
+ * M * n_out <= 2^34 (else EXFOLD_ERR_SHAPE).
  * Errors: EXFOLD_ERR_DTYPE for an unknown dtype or a bf16 output of float32 inputs;
  * EXFOLD_ERR_ARG for an unknown activation or gate flag; EXFOLD_ERR_ALIGN for pointers not
  * aligned to their element.

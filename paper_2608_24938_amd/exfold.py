@@ -494,7 +494,8 @@ def route_experts(logits, top_k, score="softmax", select_bias=None, groups=1, ke
 
 
 def linear_workspace_size(w, rows, gated=False) -> int:
-    """Bytes of workspace that linear() of `rows` rows of x and this weight needs (0: none)."""
+    """Bytes of workspace that linear() of exactly `rows` rows of x and this weight needs (0: none; fewer rows may need
+    more).  Enough for any x: one whose rows start on 16 bytes may need less."""
     ldw = _matrix(w, "w")
     n_out = w.shape[0] // 2 if gated else w.shape[0]
     code = _DTYPE[w.dtype]
@@ -509,7 +510,7 @@ def linear(x, w, bias=None, act="none", gated=False, residual=None, out_dtype=No
     bfloat16, rows contiguous; bias [n_out] (gated [2 n_out]) float32; residual and y [M, n_out] of
     out_dtype (x's type unless given; float32 is always allowed).  y may be the residual (y += ...).
     act: "none", "relu", "silu", "gelu" or "gelu_tanh".  workspace: a tensor of at least
-    linear_workspace_size bytes; made here, where one is needed, unless given.  stream: as under
+    linear_workspace_size bytes for these rows; made here, where one is needed, unless given.  stream: as under
     torch.cuda.stream(stream)."""
     ldx = _matrix(x, "x")
     dev, dtype = x.device, x.dtype
