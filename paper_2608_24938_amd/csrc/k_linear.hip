@@ -613,9 +613,10 @@ static void launch_typed(const LinearArgs &a, const LinearPlan &p, hipStream_t s
   } else if constexpr (VEC) {
     // Buffers: as many stages as two workgroups a CU leave room for where the loads are waited
     // for, few where several workgroups a CU cover each other: float32 on 32 x 64 tiles (600 x
-    // 2048 x 768: three 29.0 us, six 32.2), and 128 x 128 tiles that are more than the CUs
-    // (2048 x 4096 x 4096: two 76.2 us, four 87.6; 128 x 28672 x 4096, 224 tiles: 74.6, 63.6), and
-    // reductions of two stages on 64 x 128 tiles (5498 x 7744 x 64: two 74.5 us, three 101.6).
+    // 2048 x 768: three 29.0 us, six 32.2), 128 x 128 tiles that are more than the CUs (2048 x 4096
+    // x 4096: two 76.2 us, four 87.6; 128 x 28672 x 4096, 224 tiles: 74.6, 63.6; float32 ones are
+    // always more, the plan estimates fewer behind twice as many of 64 x 128), and reductions of
+    // two stages on 64 x 128 tiles (5498 x 7744 x 64: two 74.5 us, three 101.6).
     constexpr int S32 = sizeof(E) == 4 ? 3 : 6;
     const bool once = a.M <= p.bm;
     if (p.bm == 32 && once) linear_ring<E, 32, 64, S32, true, GATED, true><<<p.grid, 256, 0, s>>>(a, p);
@@ -624,8 +625,8 @@ static void launch_typed(const LinearArgs &a, const LinearPlan &p, hipStream_t s
     else if (p.bn == 64) linear_ring<E, 64, 64, 4, true, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.bm == 64 && p.kc <= 2 * 128 / (int)sizeof(E)) linear_ring<E, 64, 128, 2, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
     else if (p.bm == 64) linear_ring<E, 64, 128, 3, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
-    else if (p.shared_cu) linear_ring<E, 128, 128, 2, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
-    else linear_ring<E, 128, 128, 4, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+    else if (sizeof(E) == 4 || p.shared_cu) linear_ring<E, 128, 128, 2, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
+    else if constexpr (sizeof(E) == 2) linear_ring<E, 128, 128, 4, false, GATED, false><<<p.grid, 256, 0, s>>>(a, p);
   } else {
     linear_tile<E, 64, 128, GATED><<<p.grid, 256, 0, s>>>(a, p);
   }

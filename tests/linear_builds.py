@@ -29,7 +29,7 @@ def build(m, n, k, bf16=True, gated=False, x_aligned=True, ldw=None, cu=256):
     if p["kind"] == TILE:
         return ("tile",) + split
     if p["bm"] == 128:
-        kind = 2 if p["grid"] > cu else 4                          # buffers of the ring
+        kind = 2 if p["grid"] > cu or not bf16 else 4              # buffers of the ring
     elif p["bn"] == 128:
         kind = 2 if p["kc"] * esz <= 256 else 3
     else:
