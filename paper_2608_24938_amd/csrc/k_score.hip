@@ -79,8 +79,7 @@ __device__ __forceinline__ uint32_t kept_candidates(const RouteExpertsArgs &a, c
     for (int j = 1; j < R; ++j) merge(m1, m2, value[j], lowest);
     if (lanes > 1) merge(m1, m2, dpp_any<0xB1>(m1), dpp_any<0xB1>(m2));
     if (lanes > 2) merge(m1, m2, dpp_any<0x4E>(m1), dpp_any<0x4E>(m2));
-    if (lanes > 4) merge(m1, m2, dpp_any<0x141>(m1), dpp_any<0x141>(m2));
-    if (lanes > 8) merge(m1, m2, dpp_any<0x140>(m1), dpp_any<0x140>(m2));
+    if (lanes > 4) merge(m1, m2, dpp_any<0x141>(m1), dpp_any<0x141>(m2));  // at most 8: two groups or more
     const V mine = join(m1, m2);
     const uint32_t g = (uint32_t)(q / lanes);
     // rounds: the largest value of the groups that are left, then the smallest group of it
