@@ -1551,20 +1551,15 @@ hipError_t launch_plain_gemm_nt(const void *A, const void *W, int M, int N, int 
 
 // ---------------------------------------------------------------------------
 // Matrix product with an epilogue (exfold_linear_forward) on the wide tile: 256 rows x 256
-// weight rows (gated: the gate and the up rows of 128 columns).  Tiles run in panels of
-// kLinPanel m-tiles, m-tile fastest, so that the workgroups of an XCD share both operands.
+// weight rows (gated: the gate and the up rows of 128 columns), in the order of tile_of.
 // ---------------------------------------------------------------------------
-constexpr int kLinPanel = 8;
-
 template <bool GATED>
 __global__ __launch_bounds__(64 * kWideWaves, 1) void linear_wide(const LinearArgs a) {
   __shared__ __attribute__((aligned(1024))) bf16_t smem[kWideSmemElems];
   constexpr int COLS = GATED ? kWideBN / 2 : kWideBN;
   const int mts = (a.M + kWide - 1) / kWide, nts = (a.N + COLS - 1) / COLS;
-  const int L = xcd_remap(blockIdx.x, mts * nts);
-  const int panel = L / (kLinPanel * nts), in_panel = L % (kLinPanel * nts);
-  const int pm = min(kLinPanel, mts - panel * kLinPanel);
-  const int mt = panel * kLinPanel + in_panel % pm, nt = in_panel / pm;
+  int mt, nt, ks;
+  tile_of(xcd_remap(blockIdx.x, mts * nts), mts, nts, mt, nt, ks);
   const int valid = min(kWide, a.M - mt * kWide);
   const bf16_t *x = static_cast<const bf16_t *>(a.x), *w = static_cast<const bf16_t *>(a.w);
   // rows past the ends re-read the last one

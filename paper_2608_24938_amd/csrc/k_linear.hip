@@ -26,18 +26,6 @@ template <typename E> __device__ __forceinline__ void mma32(const u32x4 &a, cons
 // LDS slot (16-byte units) of piece q of tile row r (8 pieces a row).
 __device__ __forceinline__ int piece_at(int r, int q) { return r * 8 + (q ^ ((r ^ (r >> 1)) & 7)); }
 
-// Tile of logical id L: panels of kPanel m-tiles, m-tile fastest in a panel, then the n-tiles, then
-// the panels, then the splits, so that an XCD's consecutive ids share rows and weights (8192 x
-// 1024 x 4096 83.6 -> 78.4 us against all m-tiles first).
-constexpr int kPanel = 8;
-__device__ __forceinline__ void tile_of(int L, int mts, int nts, int &mt, int &nt, int &ks) {
-  ks = L / (mts * nts);
-  L -= ks * mts * nts;
-  const int panel = L / (kPanel * nts), in = L - panel * kPanel * nts, pm = min(kPanel, mts - panel * kPanel);
-  nt = in / pm;
-  mt = panel * kPanel + in - nt * pm;
-}
-
 // A wave's TM x TN tiles of sums into LDS, row-major: register r of tile (i, j) is row arow(i) +
 // lane % 32, column brow(j) + 8 (r / 4) + 4 (lane / 32) + r % 4 (the weights are the MFMA's first
 // operand): runs of four columns.
