@@ -400,6 +400,9 @@ exfold_status exfold_calibrate_diagonal(const exfold_layer *layer, const void *x
  * Weights.  p_e (0 for a masked expert); with renorm divided by their sum over the K
  *           routes (all 0 when that sum is 0); times scale.  Evaluated in float64 and
  *           rounded once to float32.
+ * Calibration takes no given routes: in the co-routed mode exfold_calibrate_projectors and
+ * exfold_calibrate_diagonal pair experts by the layer's own Top-K softmax, whatever router the
+ * model is served with; EXFOLD_CAL_COMMON pairs all experts and depends on no router.
  */
 enum { EXFOLD_SCORE_SOFTMAX = 0, EXFOLD_SCORE_SIGMOID = 1 };
 enum { EXFOLD_GROUP_MAX = 0, EXFOLD_GROUP_TOP2 = 1 };

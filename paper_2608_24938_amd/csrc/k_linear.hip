@@ -327,7 +327,7 @@ __global__ __launch_bounds__(256, BM == 128 && S > 2 ? 1 : 2) void linear_ring(c
 // rows) over the whole reduction, its 256 threads on consecutive 16-byte pieces of each (VEC:
 // the rows start on 16 bytes and hold whole pieces), two sweeps of loads in flight, products
 // in float32 on the vector units; the threads' sums are added by DPP within rows of 16 lanes
-// and then in order through LDS.  One token, 2 x 1408 weight rows of 4096: 6.0 us, 3.9 TB/s.
+// and then in order through LDS.  One token, 2 x 1408 weight rows of 4096: 5.6 us, 4.1 TB/s.
 // ---------------------------------------------------------------------------
 // Elements of a 16-byte piece as float32.
 template <typename E> __device__ __forceinline__ void unpack_piece(const u32x4 &v, float (&f)[16 / sizeof(E)]) {
@@ -485,9 +485,11 @@ __global__ __launch_bounds__(256) void linear_copy(const LinearArgs a, const E *
 // The tile and split of the least estimated time: rounds of tiles over the CUs, or the
 // weights' and rows' bytes from memory (about 4.8 TB/s) where those take longer, and for a
 // split its partial sums, written and read, and the launch that joins them.  The estimate
-// picks among kernels that all are right (600 x 2048 x 768 float32: 29 us on 32 x 64 tiles, 33
-// on 64 x 128 and 34 on 128 x 128; 777 x 1408 x 1024 bf16: 15.5, 13.4, 19.7, and 12.4 on 64 x
-// 64; 64 x 4096 x 4096 bf16: 13.4 us split in four, 15.3 not).
+// picks among kernels that all are right (600 x 2048 x 768 float32: taken 32 x 64 tiles, 29 us, 64 x
+// 128 33 and 128 x 128 34; 64 x 4096 x 4096 bf16: taken a split in four, 13.4 us, none 15.3).  It
+// charges a whole round for every cu_count ring tiles, though two of 64 x 64 share a CU, and so
+// passes over them where they are a few more than the CUs (777 x 1408 x 1024 bf16: taken 64 x 128,
+// 13.4 us, 64 x 64 12.4, 32 x 64 15.5, 128 x 128 19.7).
 static double plan_tiles(bool bf16, bool gated, bool vec, int M, int N, int K, int cu_count, LinearPlan &p) {
   p = LinearPlan{};
   p.vec = vec;

@@ -140,8 +140,8 @@ __device__ __forceinline__ uint32_t kept_candidates(const RouteExpertsArgs &a, c
 // Scores of all experts are computed where something needs them (SC: a bias, or groups by
 // their two largest; a softmax that is not renormalised needs its sum), else those of the K
 // routes only.
-// Bound by its instructions: 65536 tokens of 256 experts, bf16, in 8 groups 28 us (58 us with
-// whole-key rounds and groups through LDS; the bytes take 7), 8192 of 128 with a bias 10.4 us.
+// Bound by its instructions: 65536 tokens of 256 experts, bf16, in 8 groups 26.8 us (58 us with
+// whole-key rounds and groups through LDS; the bytes take 7), 8192 of 128 with a bias 9.3 us.
 template <typename E, int R, bool BIAS, bool SC>
 __global__ __launch_bounds__(256) void route_experts_kernel(const RouteExpertsArgs a) {
   static_assert(SC || !BIAS, "a bias needs the scores");
