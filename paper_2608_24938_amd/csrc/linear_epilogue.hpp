@@ -31,8 +31,8 @@ template <bool FAST> __device__ __forceinline__ float sigmoid_times(float z, flo
 // rounded z / sqrt(2) has the z^2 too): Phi(-m) = exp(-m^2 / 2) times half the scaled complementary
 // error function of m / sqrt(2), which is smooth in t = 1 / (1 + m / (2 sqrt(2))): a polynomial of
 // degree 9 without constant term, fitted to least relative error over m < 13.3 (9e-8 with its
-// float32 coefficients).  Of 2e7 normal z, 2.0e-5 round to another bf16 than the exact value (a
-// degree of 7: 9.4e-5).  8192 x 8192 outputs of 512-long rows: 126.0 us, 122.6 with degree 7; 777 x
+// float32 coefficients).  Of 2e7 normal z, 2.0e-5 round to another bf16 than the exact value in a
+// float32 model of it (a degree of 7: 9.4e-5).  8192 x 8192 outputs of 512-long rows: 126.0 us, 122.6 with degree 7; 777 x
 // 1408 outputs of 64-long rows: 6.3 us, 8.7 with the library's function, 5.0 without an activation.
 __device__ __forceinline__ float gelu_few_ulps(float z) {
   // beyond 16 Phi(-m) is 0 in float32, and an infinite m would make 0 * m of it
